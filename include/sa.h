@@ -28,6 +28,11 @@
  * and the cache-reuse decision:
  *  10. sa_cache_indicator           -- synchronization-aware cache-reuse
  *                                      indicator (Sec. 4.3, Eq. (12)-(15)).
+ * Beside the layer, for generation chunk by chunk:
+ *  11. sa_pages_reserve, _write, _fork, _free, _compact, _copy
+ *                                   -- keys and values kept in pages;
+ *  12. sa_prefix_attention          -- the attention that reads them, keys that
+ *                                      sequences share taken once for all.
  *
  * Conventions shared by every call
  * --------------------------------
@@ -420,6 +425,159 @@ int sa_cache_indicator(const void* y_v, const void* y_v_hat,
                        int dtype, float lambda_p, float lambda_s, float tau,
                        float eps, float* out, void* ws, size_t ws_bytes,
                        void* stream);
+
+/*
+ * Keys and values kept in pages, and the attention that reads them.
+ *
+ * A cache holds the keys and values of up to B sequences: samples of one or
+ * several prompts or clips that are generated chunk by chunk or token by token.
+ *   k_pages, v_pages  [n_pages,Hkv,page,d] in dtype, one pair a layer
+ *   page_table        [B,max_pages] i32: page of tokens page*j .. of a sequence;
+ *                     -1 = none
+ *   seq_len           [B] i32: tokens of each sequence (negative counts as 0)
+ *   page_ref          [n_pages] i32: how many table entries name the page; 0 = free
+ * page in {16, 32, 64, 128}; max_pages * page <= 2^30; B <= 16384 (the attention:
+ * B + n_groups <= 1024).  Every list lives on the device, so the calls can be
+ * captured into a HIP graph and follow the lists' values at each replay.  Calls
+ * on one cache that may overlap in time must be ordered by the caller.
+ */
+
+/*
+ * sa_pages_reserve -- pages for n_new[b] more tokens of every sequence, and
+ * seq_len[b] += n_new[b].
+ *
+ * Pages are handed out lowest number first, to the sequences in order, to each
+ * in the order of its tokens.  All or nothing: with too few free pages, or a
+ * sequence that would outgrow its table row, nothing is changed and missing[0]
+ * is the number of pages and table entries that lack; otherwise it is 0.  The
+ * page that holds a sequence's last tokens must not be shared if it has room
+ * left (sa_pages_fork leaves none so).
+ *
+ *   n_new      [B] i32 in (negative counts as 0)
+ *   missing    [1] i32 out
+ */
+int sa_pages_reserve(int32_t* page_table, int32_t* seq_len, int32_t* page_ref,
+                     const int32_t* n_new, int B, int max_pages, int n_pages,
+                     int page, int32_t* missing, void* stream);
+
+/*
+ * sa_pages_write -- the keys and values of each sequence's last n_new[b] tokens
+ * (those that sa_pages_reserve made room for) into one layer's pages: row s of
+ * sequence b is token seq_len[b] - n_new[b] + s.
+ *
+ *   k, v       [B,Hkv,S,d] in dtype; not overlapping the pages
+ *   n_new      [B] i32, at most S count; NULL = S for every sequence.  Rows from
+ *              n_new[b] on are not read, and tokens without a page not written.
+ */
+int sa_pages_write(const void* k, const void* v, void* k_pages, void* v_pages,
+                   const int32_t* page_table, const int32_t* seq_len,
+                   const int32_t* n_new, int B, int Hkv, int S, int d,
+                   int dtype, int n_pages, int page, int max_pages,
+                   void* stream);
+
+/*
+ * sa_pages_fork -- sequence dst[i] becomes a copy of sequence src[i], i < n.
+ *
+ * The full pages are shared (an owner more each).  A partial last page gets a
+ * fresh page, so that both sequences can go on writing: the pair (copy_src[i],
+ * copy_dst[i]) is to be copied in every pool with sa_pages_copy before either is
+ * written; both are -1 where there is nothing to copy.  An entry whose src has
+ * no tokens, whose dst has some, or that names a sequence outside [0,B) is left
+ * out, and of several entries with one dst the first counts.  Fresh pages are
+ * the lowest free ones, in the order of the entries; with too few nothing is
+ * changed, missing[0] is how many lack (otherwise 0), and all pairs are -1.
+ *
+ *   src, dst            [n] i32, 1 <= n <= B
+ *   copy_src, copy_dst  [n] i32 out
+ *   missing             [1] i32 out
+ */
+int sa_pages_fork(int32_t* page_table, int32_t* seq_len, int32_t* page_ref,
+                  const int32_t* src, const int32_t* dst, int n, int B,
+                  int max_pages, int n_pages, int page, int32_t* copy_src,
+                  int32_t* copy_dst, int32_t* missing, void* stream);
+
+/*
+ * sa_pages_free -- the n sequences seqs[i] give up their pages: every page of
+ * theirs has an owner less, their table rows are -1, their lengths 0.  Numbers
+ * outside [0,B) are left out, and a number named twice counts once.
+ *
+ *   seqs       [n] i32, 1 <= n <= 16384
+ */
+int sa_pages_free(int32_t* page_table, int32_t* seq_len, int32_t* page_ref,
+                  const int32_t* seqs, int n, int B, int max_pages,
+                  int n_pages, int page, void* stream);
+
+/*
+ * sa_pages_compact -- the pages in use become the first ones: with U of them,
+ * the k-th used page from number U on (ascending) moves to the k-th free page
+ * below U.  page_table and page_ref are rewritten; the pages themselves move
+ * with sa_pages_copy(move_src, move_dst) in every pool, before anything else
+ * uses them.
+ *
+ *   move_src, move_dst  [n_pages / 2] i32 out, -1 behind the moves
+ *   counts              [2] i32 out: U, number of moves
+ */
+int sa_pages_compact(int32_t* page_table, int32_t* page_ref, int B,
+                     int max_pages, int n_pages, int32_t* move_src,
+                     int32_t* move_dst, int32_t* counts, void* stream);
+
+/*
+ * sa_pages_copy -- page src[i] over page dst[i] in every pool, i < n.  Pairs
+ * with a number outside [0,n_pages) are left out.  A page may be the source of
+ * several pairs; no page may be the destination of two pairs, or of one and the
+ * source of another (the pairs of sa_pages_fork and sa_pages_compact are so).
+ *
+ *   pools       [n_pools,n_pages,page_bytes] (K and V of all layers in one
+ *               allocation, or one of them at a time), 16-byte aligned
+ *   page_bytes  Hkv * page * d * element size: a multiple of 16, at most 2^31
+ *   src, dst    [n] i32; n = 0: nothing to do
+ */
+int sa_pages_copy(void* pools, int n_pools, int n_pages, size_t page_bytes,
+                  const int32_t* src, const int32_t* dst, int n, void* stream);
+
+/*
+ * sa_prefix_attention -- attention of every sequence's newest queries over its
+ * pages; the keys that the sequences of a group share are read once for all.
+ *
+ * O = softmax(Q K^T * scale) V and lse over tokens 0 .. seq_len[b]-1 of each
+ * sequence.  Query s of sequence b is its token seq_len[b] - q_len[b] + s; with
+ * causal = 1 it sees the tokens up to its own only.  Query head i reads key head
+ * i / (Hq / Hkv).  A row that sees no key outputs zeros and lse = -inf, as does
+ * one whose every logit is -inf; rows from q_len[b] on are left as they were.
+ * Tokens whose table entry is no page are left out, and nothing that lies in a
+ * page behind a sequence's last token is used.  A token that a query does not
+ * see by causality weighs 0 in it: its value must be finite.
+ *
+ * The B sequences are n_groups groups of B / n_groups neighbours.  shared_len[g]
+ * says how many leading tokens the sequences of group g have in common, in the
+ * same pages (as sa_pages_fork leaves them); the call uses the whole pages among
+ * them that every sequence of the group with a token has (and, causal, that
+ * every query sees), and reads them through the first such sequence's row.  It
+ * is a statement about the pages, not a mask: the result is that of n_groups = 0
+ * up to the order of the sums.
+ *
+ *   q          [B,Hq,S,d] in dtype, S <= 262144
+ *   o          [B,Hq,S,d] in/out in dtype (round to nearest even from fp32; with
+ *              bf16 the softmax weights are rounded to bf16 before they multiply
+ *              V, the row sums are fp32)
+ *   lse        [B,Hq,S] f32 in/out, natural log, nullable
+ *   shared_len [n_groups] i32, NULL iff n_groups = 0
+ *   q_len      [B] i32 (clamped to [0,S]), NULL = S for every sequence
+ *   Hq         a multiple of Hkv
+ *   ws         workspace of at least sa_prefix_attention_workspace(...) bytes
+ */
+int sa_prefix_attention(const void* q, const void* k_pages,
+                        const void* v_pages, void* o, float* lse,
+                        const int32_t* page_table, const int32_t* seq_len,
+                        const int32_t* shared_len, const int32_t* q_len, int B,
+                        int Hq, int Hkv, int S, int d, int dtype, float scale,
+                        int causal, int n_groups, int n_pages, int page,
+                        int max_pages, void* ws, size_t ws_bytes,
+                        void* stream);
+
+/* Workspace bytes of sa_prefix_attention (0 for sizes that it rejects). */
+size_t sa_prefix_attention_workspace(int B, int Hq, int Hkv, int S, int d,
+                                     int dtype, int n_groups);
 
 /*
  * Workspace bytes of a call (SA_CALL_*) at the given sizes (the least it

@@ -21,6 +21,8 @@ Sparse Attention"):
   Eq. (11) with protected query tokens (dense rows over the block pattern);
 * ``cache``      -- Eq. (12)-(15): the synchronization-aware cache-reuse
   indicator (relative L1 changes, protected-row change, saliency drift);
+* ``pages``      -- keys and values in pages (reserve, fork, free, compact) and the
+  attention that reads them;
 * ``layer``      -- the steps composed: the video layer with protected blocks,
   token-protected sparse self-attention of either modality (Eq. (8)-(11),
   m in {v, a}; the audio branch with the audio-token saliency), and the two
@@ -41,6 +43,7 @@ from .layer import (protected_sparse_layer, modality_protected_layer,
 from .tokens import (saliency_ema, select_protected_tokens,
                      token_protected_attention, token_protected_rows)
 from .cache import relative_l1, saliency_drift, cache_indicator
+from . import pages
 
 __all__ = [
     "cross_scores", "token_to_block_saliency", "topk_order",
@@ -50,5 +53,5 @@ __all__ = [
     "modality_protected_layer", "cross_attention_with_saliency",
     "computed_flops", "dense_flops", "saliency_ema", "select_protected_tokens",
     "token_protected_attention", "token_protected_rows", "relative_l1",
-    "saliency_drift", "cache_indicator",
+    "saliency_drift", "cache_indicator", "pages",
 ]

@@ -8,7 +8,9 @@ attention; beside it the lagged saliency update and token-granular protection
 with the saliency taken from their row log-sum-exps, the mask's block means
 pooled inside the saliency streams (``sa_cross_scores_pooled`` +
 ``sa_build_block_mask_pooled``), and the
-synchronization-aware cache-reuse indicator (Sec. 4.3).  Everything runs in
+synchronization-aware cache-reuse indicator (Sec. 4.3); for generation chunk by
+chunk, keys and values kept in pages (``sa_pages_*``) and the attention over
+them that takes shared tokens once for a group (``sa_prefix_attention``).  Everything runs in
 hand-written HIP kernels behind a C ABI (``include/sa.h``, ``libsa.so``); this
 package is a thin ctypes binding over it.
 """
@@ -19,6 +21,8 @@ from .binding import (  # noqa: F401
     sa_cache_indicator, SA_CALL_CACHE_INDICATOR, SA_CALL_TOKEN_ATTENTION,
     sa_cross_attention, sa_cross_scores_from_lse, SA_CALL_CROSS_ATTENTION,
     sa_pool_columns, sa_cross_scores_pooled, sa_build_block_mask_pooled,
+    sa_pages_reserve, sa_pages_write, sa_pages_fork, sa_pages_free, sa_pages_compact,
+    sa_pages_copy, sa_prefix_attention, sa_prefix_attention_workspace,
     SA_BF16, SA_F32, SA_CALL_CROSS_SCORES, SA_CALL_BUILD_BLOCK_MASK,
     SA_CALL_SPARSE_ATTENTION, SA_CALL_SELECT_PROTECTED, SA_OK,
     SA_ERR_INVALID_ARG, SA_ERR_UNSUPPORTED, SA_ERR_WORKSPACE, SA_ERR_HIP,

@@ -52,6 +52,16 @@ SIGNATURES = {
                                     _F, _I, _VP, _VP, _VP, _I, _VP, _VP, _VP, _SZ, _VP]),
     "sa_build_block_mask_pooled": (_I, [_VP, _VP, _I, _I, _I, _I, _F, _I, _I, _VP, _VP, _VP,
                                         _VP, _VP, _VP]),
+    "sa_pages_reserve": (_I, [_VP, _VP, _VP, _VP, _I, _I, _I, _I, _VP, _VP]),
+    "sa_pages_write": (_I, [_VP, _VP, _VP, _VP, _VP, _VP, _VP, _I, _I, _I, _I, _I, _I, _I, _I,
+                            _VP]),
+    "sa_pages_fork": (_I, [_VP, _VP, _VP, _VP, _VP, _I, _I, _I, _I, _I, _VP, _VP, _VP, _VP]),
+    "sa_pages_free": (_I, [_VP, _VP, _VP, _VP, _I, _I, _I, _I, _I, _VP]),
+    "sa_pages_compact": (_I, [_VP, _VP, _I, _I, _I, _VP, _VP, _VP, _VP]),
+    "sa_pages_copy": (_I, [_VP, _I, _I, _SZ, _VP, _VP, _I, _VP]),
+    "sa_prefix_attention": (_I, [_VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _I, _I, _I, _I,
+                                 _I, _I, _F, _I, _I, _I, _I, _I, _VP, _SZ, _VP]),
+    "sa_prefix_attention_workspace": (_SZ, [_I, _I, _I, _I, _I, _I, _I]),
     "sa_workspace_size": (_SZ, [_I, _I, _I, _I, _I, _I, _I]),
     "sa_last_error": (ctypes.c_char_p, []),
     "sa_version": (_I, []),
@@ -481,6 +491,180 @@ def sa_cache_indicator(y_v, y_v_hat, *, prot_flag=None, y_a=None, y_a_hat=None,
         float(lambda_s), float(tau), float(eps), _ptr(out), _ptr(ws), _nbytes(ws),
         _stream()))
     return out
+
+
+# ---- pages of keys and values ----------------------------------------------
+def _here(*tensors):
+    """The calls go to the current device's current stream: a tensor of another
+    device is refused."""
+    dev = tensors[0].device
+    for t in tensors:
+        if t is not None and t.device != dev:
+            raise ValueError(f"tensors on {dev} and {t.device}")
+    if dev.type == "cuda" and dev.index != torch.cuda.current_device():
+        raise ValueError(f"tensors on {dev}, which is not the current device")
+    return dev
+
+
+def _table(page_table, seq_len, page_ref=None):
+    """B and max_pages of a page table; its lists' shapes and types are checked."""
+    if page_table.dim() != 2:
+        raise ValueError(f"page_table: shape {tuple(page_table.shape)}, expected [B, max_pages]")
+    B, max_pages = page_table.shape
+    _expect(page_table, "page_table", (B, max_pages), torch.int32)
+    _expect(seq_len, "seq_len", (B,), torch.int32)
+    if page_ref is not None:
+        _expect(page_ref, "page_ref", (page_ref.numel(),), torch.int32)
+    return B, max_pages
+
+
+def sa_pages_reserve(page_table, seq_len, page_ref, n_new, page, *, missing=None):
+    """Pages for n_new[b] more tokens of every sequence, in place; returns
+    missing [1] i32 (0 = done, else nothing was changed)."""
+    B, max_pages = _table(page_table, seq_len, page_ref)
+    _expect(n_new, "n_new", (B,), torch.int32)
+    _expect(missing, "missing", (1,), torch.int32)
+    dev = _here(page_table, seq_len, page_ref, n_new, missing)
+    if missing is None:
+        missing = torch.empty(1, dtype=torch.int32, device=dev)
+    _check(lib().sa_pages_reserve(
+        _ptr(page_table), _ptr(seq_len), _ptr(page_ref), _ptr(n_new), B, max_pages,
+        page_ref.numel(), int(page), _ptr(missing), _stream()))
+    return missing
+
+
+def sa_pages_write(k, v, k_pages, v_pages, page_table, seq_len, *, n_new=None):
+    """The last n_new[b] tokens' rows of k, v [B,Hkv,S,d] into the pages
+    [n_pages,Hkv,page,d]; returns (k_pages, v_pages)."""
+    B, Hkv, S, d = k.shape
+    n_pages, _, page, _ = k_pages.shape
+    _table(page_table, seq_len)
+    _expect(v, "v", (B, Hkv, S, d), k.dtype)
+    _expect(k_pages, "k_pages", (n_pages, Hkv, page, d), k.dtype)
+    _expect(v_pages, "v_pages", (n_pages, Hkv, page, d), k.dtype)
+    _expect(seq_len, "seq_len", (B,), torch.int32)
+    _expect(n_new, "n_new", (B,), torch.int32)
+    _here(k, v, k_pages, v_pages, page_table, seq_len, n_new)
+    _check(lib().sa_pages_write(
+        _ptr(k), _ptr(v), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(seq_len),
+        _ptr(n_new), B, Hkv, S, d, _dtype_code(k), n_pages, page, page_table.shape[1],
+        _stream()))
+    return k_pages, v_pages
+
+
+def sa_pages_fork(page_table, seq_len, page_ref, src, dst, page, *, copy_src=None,
+                  copy_dst=None, missing=None):
+    """Sequences dst become copies of sequences src, in place; returns (copy_src,
+    copy_dst, missing): the pages to copy in every pool (-1 = none)."""
+    B, max_pages = _table(page_table, seq_len, page_ref)
+    n = src.numel()
+    for name, t in (("src", src), ("dst", dst), ("copy_src", copy_src), ("copy_dst", copy_dst)):
+        _expect(t, name, (n,), torch.int32)
+    _expect(missing, "missing", (1,), torch.int32)
+    dev = _here(page_table, seq_len, page_ref, src, dst, copy_src, copy_dst, missing)
+    if copy_src is None:
+        copy_src = torch.empty(n, dtype=torch.int32, device=dev)
+    if copy_dst is None:
+        copy_dst = torch.empty(n, dtype=torch.int32, device=dev)
+    if missing is None:
+        missing = torch.empty(1, dtype=torch.int32, device=dev)
+    _check(lib().sa_pages_fork(
+        _ptr(page_table), _ptr(seq_len), _ptr(page_ref), _ptr(src), _ptr(dst), n, B, max_pages,
+        page_ref.numel(), int(page), _ptr(copy_src), _ptr(copy_dst), _ptr(missing), _stream()))
+    return copy_src, copy_dst, missing
+
+
+def sa_pages_free(page_table, seq_len, page_ref, seqs, page):
+    """The sequences of seqs give up their pages, in place."""
+    B, max_pages = _table(page_table, seq_len, page_ref)
+    n = seqs.numel()
+    _expect(seqs, "seqs", (n,), torch.int32)
+    _here(page_table, seq_len, page_ref, seqs)
+    _check(lib().sa_pages_free(
+        _ptr(page_table), _ptr(seq_len), _ptr(page_ref), _ptr(seqs), n, B, max_pages,
+        page_ref.numel(), int(page), _stream()))
+
+
+def sa_pages_compact(page_table, page_ref, *, move_src=None, move_dst=None, counts=None):
+    """The pages in use become the first ones, in place; returns (move_src,
+    move_dst [n_pages // 2], counts [2]): the moves for sa_pages_copy (-1 behind
+    them), pages in use and moves."""
+    B, max_pages = _table(page_table, None, page_ref)
+    n_pages = page_ref.numel()
+    _expect(move_src, "move_src", (n_pages // 2,), torch.int32)
+    _expect(move_dst, "move_dst", (n_pages // 2,), torch.int32)
+    _expect(counts, "counts", (2,), torch.int32)
+    dev = _here(page_table, page_ref, move_src, move_dst, counts)
+    if move_src is None:
+        move_src = torch.empty(n_pages // 2, dtype=torch.int32, device=dev)
+    if move_dst is None:
+        move_dst = torch.empty(n_pages // 2, dtype=torch.int32, device=dev)
+    if counts is None:
+        counts = torch.empty(2, dtype=torch.int32, device=dev)
+    _check(lib().sa_pages_compact(
+        _ptr(page_table), _ptr(page_ref), B, max_pages, n_pages,
+        _ptr(move_src) if n_pages > 1 else None, _ptr(move_dst) if n_pages > 1 else None,
+        _ptr(counts), _stream()))
+    return move_src, move_dst, counts
+
+
+def sa_pages_copy(pools, src, dst):
+    """Page src[i] over page dst[i] in every pool of pools [n_pools,n_pages,...];
+    returns pools."""
+    if pools.dim() < 3:
+        raise ValueError(f"pools: shape {tuple(pools.shape)}, expected [n_pools, n_pages, ...]")
+    n_pools, n_pages = pools.shape[:2]
+    n = src.numel()
+    _expect(src, "src", (n,), torch.int32)
+    _expect(dst, "dst", (n,), torch.int32)
+    _here(pools, src, dst)
+    _check(lib().sa_pages_copy(
+        _ptr(pools), n_pools, n_pages, pools.stride(1) * pools.element_size(),
+        _ptr(src) if n > 0 else None, _ptr(dst) if n > 0 else None, n, _stream()))
+    return pools
+
+
+def sa_prefix_attention_workspace(B: int, Hq: int, Hkv: int, S: int, d: int, dtype,
+                                  n_groups: int = 0) -> int:
+    """Workspace bytes of sa_prefix_attention."""
+    code = {torch.bfloat16: SA_BF16, torch.float32: SA_F32}.get(dtype, -1)
+    return int(lib().sa_prefix_attention_workspace(B, Hq, Hkv, S, d, code, n_groups))
+
+
+def sa_prefix_attention(q, k_pages, v_pages, page_table, seq_len, scale, *, shared_len=None,
+                        q_len=None, causal=False, o=None, lse=None, want_lse=False, ws=None):
+    """Attention of q [B,Hq,S,d] over the sequences' pages [n_pages,Hkv,page,d], the
+    first shared_len[g] tokens of each group taken once for all its sequences; returns
+    (o, lse).  Rows from q_len[b] on are left as they were: in an o or lse that is made
+    here they are zeros."""
+    B, Hq, S, d = q.shape
+    n_pages, Hkv, page, _ = k_pages.shape
+    _table(page_table, seq_len)
+    _expect(page_table, "page_table", (B, page_table.shape[1]), torch.int32)
+    _expect(k_pages, "k_pages", (n_pages, Hkv, page, d), q.dtype)
+    _expect(v_pages, "v_pages", (n_pages, Hkv, page, d), q.dtype)
+    _expect(o, "o", (B, Hq, S, d), q.dtype)
+    _expect(lse, "lse", (B, Hq, S), torch.float32)
+    _expect(q_len, "q_len", (B,), torch.int32)
+    n_groups = 0
+    if shared_len is not None:
+        n_groups = shared_len.numel()
+        _expect(shared_len, "shared_len", (n_groups,), torch.int32)
+    dev = _here(q, k_pages, v_pages, page_table, seq_len, shared_len, q_len, o, lse, ws)
+    make = torch.empty if q_len is None else torch.zeros
+    if o is None:
+        o = make(B, Hq, S, d, dtype=q.dtype, device=dev)
+    if lse is None and want_lse:
+        lse = make(B, Hq, S, dtype=torch.float32, device=dev)
+    if ws is None:
+        need = sa_prefix_attention_workspace(B, Hq, Hkv, S, d, q.dtype, n_groups)
+        ws = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
+    _check(lib().sa_prefix_attention(
+        _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(o), _ptr(lse), _ptr(page_table),
+        _ptr(seq_len), _ptr(shared_len), _ptr(q_len), B, Hq, Hkv, S, d, _dtype_code(q),
+        float(scale), int(bool(causal)), n_groups, n_pages, page, page_table.shape[1], _ptr(ws),
+        _nbytes(ws), _stream()))
+    return o, lse
 
 
 # ---- measurement helper library (libsa_bench.so, include/sa_bench.h) --------

@@ -2,14 +2,12 @@
 // reporting, dispatch to the kernel launchers.  Every check runs on the host
 // before any launch, so a rejected call writes nothing.
 #include <math.h>
-#include <stdarg.h>
-#include <stdio.h>
 
 #include <algorithm>
 #include <mutex>
-#include <string>
 
 #include "../../include/sa.h"
+#include "sa_checks.h"
 #include "sa_device.h"
 #include "sa_internal.h"
 
@@ -23,39 +21,13 @@ constexpr size_t kStaticSplitBytes =
               sa::attn_split_bytes(64, 128), sa::attn_split_bytes(64, 64)});
 static __device__ __align__(256) unsigned char scratch[kStaticScratchBytes + kStaticSplitBytes];
 
+using namespace sa::host;
+
 namespace {
 
 constexpr int kMaxScratchDevices = 64;
 std::mutex g_scratch_mutex;
 char* g_scratch_ptr[kMaxScratchDevices];  // device address of scratch, per device
-
-thread_local std::string g_last_error;
-
-int fail(int code, const char* fmt, ...) {
-  char buf[512];
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(buf, sizeof(buf), fmt, ap);
-  va_end(ap);
-  g_last_error = buf;
-  return code;
-}
-
-int ok() {
-  g_last_error.clear();
-  return SA_OK;
-}
-
-int check_launch(const char* what) {
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess)
-    return fail(SA_ERR_HIP, "%s: kernel launch failed: %s", what, hipGetErrorString(e));
-  return ok();
-}
-
-bool aligned(const void* p, size_t a) {
-  return (reinterpret_cast<uintptr_t>(p) % a) == 0;
-}
 
 // Shared shape checks; returns SA_OK or an error code with the message set.
 int check_common(const char* fn, int B, int H, int L, int d, int dtype, float scale,
@@ -81,36 +53,9 @@ int check_common(const char* fn, int B, int H, int L, int d, int dtype, float sc
   return SA_OK;
 }
 
-int check_tensor(const char* fn, const char* name, const void* p, bool required,
-                 size_t align) {
-  if (p == nullptr) {
-    if (required) return fail(SA_ERR_INVALID_ARG, "%s: %s is NULL", fn, name);
-    return SA_OK;
-  }
-  if (!aligned(p, align))
-    return fail(SA_ERR_INVALID_ARG, "%s: %s is not %zu-byte aligned", fn, name, align);
-  return SA_OK;
-}
-
-int check_ws(const char* fn, const void* ws, size_t ws_bytes, size_t need) {
-  if (ws_bytes < need)
-    return fail(SA_ERR_WORKSPACE, "%s: workspace of %zu bytes is below the %zu required",
-                fn, ws_bytes, need);
-  if (need > 0 && ws == nullptr) return fail(SA_ERR_INVALID_ARG, "%s: ws is NULL", fn);
-  if (need > 0 && !aligned(ws, 16))
-    return fail(SA_ERR_INVALID_ARG, "%s: ws is not 16-byte aligned", fn);
-  return SA_OK;
-}
-
 #ifndef SA_SRC_ID
 #define SA_SRC_ID "unknown"
 #endif
-
-#define SA_TRY(expr)          \
-  do {                        \
-    const int rc_ = (expr);   \
-    if (rc_ != SA_OK) return rc_; \
-  } while (0)
 
 int check_sparse_attention_args(const char* fn, const void* q, const void* k, const void* v,
                                 const void* o, const float* lse, int B, int H, int L, int d,
@@ -187,7 +132,7 @@ int sa_version(void) { return 100; }
 
 const char* sa_build_id(void) { return SA_SRC_ID; }
 
-const char* sa_last_error(void) { return g_last_error.c_str(); }
+const char* sa_last_error(void) { return last_error().c_str(); }
 
 size_t sa_workspace_size(int call, int B, int H, int L_v, int L_a, int d, int block) {
   if (call == SA_CALL_CACHE_INDICATOR)

@@ -277,4 +277,65 @@ void launch_sparse_attention_f32(const float* q, const float* k,
                                  const int32_t* kv_idx, const int32_t* kv_cnt,
                                  char* ws, hipStream_t s);
 
+// ---- pages of keys and values ---------------------------------------------
+constexpr int kMaxSequences = 16384;  // sequences of a page table
+void launch_pages_reserve(int32_t* table, int32_t* seq_len, int32_t* ref, const int32_t* n_new,
+                          int B, int max_pages, int n_pages, int page, int32_t* missing,
+                          hipStream_t s);
+void launch_pages_fork(int32_t* table, int32_t* seq_len, int32_t* ref, const int32_t* src,
+                       const int32_t* dst, int n, int B, int max_pages, int n_pages, int page,
+                       int32_t* copy_src, int32_t* copy_dst, int32_t* missing, hipStream_t s);
+void launch_pages_free(int32_t* table, int32_t* seq_len, int32_t* ref, const int32_t* seqs, int n,
+                       int B, int max_pages, int n_pages, int page, hipStream_t s);
+void launch_pages_compact(int32_t* table, int32_t* ref, int B, int max_pages, int n_pages,
+                          int32_t* move_src, int32_t* move_dst, int32_t* counts, hipStream_t s);
+void launch_pages_copy(void* pools, int n_pools, int n_pages, size_t page_bytes,
+                       const int32_t* src, const int32_t* dst, int n, hipStream_t s);
+void launch_pages_write(const void* k, const void* v, void* k_pages, void* v_pages,
+                        const int32_t* table, const int32_t* seq_len, const int32_t* n_new, int B,
+                        int Hkv, int S, int row_bytes, int max_pages, int n_pages, int page,
+                        hipStream_t s);
+
+// Attention over pages.  The arguments of sa_prefix_attention but for d, dtype, the
+// workspace and the stream.
+struct PrefixCall {
+  const void *q, *k_pages, *v_pages;
+  void* o;
+  float* lse;
+  const int32_t *page_table, *seq_len, *shared_len, *q_len;
+  int B, Hq, Hkv, S, n_groups, n_pages, page, max_pages, causal;
+  float scale;
+};
+constexpr int kMaxAttendSegs = 1024;  // sequences and groups of a call
+constexpr int kPrefixSlots = 2 * kXcds * kCusPerXcd;  // workgroups at once, two a CU
+
+struct PrefixWs {
+  int groups;       // groups whose shared keys are taken once (0: every sequence by itself)
+  int shared_rows;  // rows of a row tile: shared keys,
+  int own_rows;     // own keys,
+  int piece_rows;   // and of a partial row tile's place
+  size_t sched, sched_sh;   // int64 [kMaxAttendSegs + 1], int [kMaxAttendSegs / 2]
+  size_t full, full_ml;     // float [2][B*Hq*S][d], float2 [2][B*Hq*S]; with groups only
+  size_t piece, piece_ml;   // float [2 slots][piece_rows][d], float2 [2 slots][piece_rows]
+  size_t total;
+};
+inline PrefixWs prefix_ws_layout(int B, int Hq, int Hkv, int S, int d, int dtype, int n_groups) {
+  PrefixWs w{};
+  const long long RS = static_cast<long long>(Hq / Hkv) * S;
+  w.groups = n_groups > 0 && B > n_groups && RS < 128 ? n_groups : 0;
+  w.shared_rows = w.own_rows = w.piece_rows = dtype == 0 ? 32 : 16;
+  const size_t rows = static_cast<size_t>(B) * Hq * S;
+  size_t off = 0;
+  w.sched = off;    off += align_up(sizeof(long long) * (kMaxAttendSegs + 1));
+  w.sched_sh = off; off += align_up(sizeof(int) * (kMaxAttendSegs / 2));
+  w.full = off;     off += w.groups > 0 ? align_up(sizeof(float) * 2 * rows * d) : 0;
+  w.full_ml = off;  off += w.groups > 0 ? align_up(sizeof(float) * 4 * rows) : 0;
+  const size_t places = static_cast<size_t>(2) * kPrefixSlots * w.piece_rows;
+  w.piece = off;    off += align_up(sizeof(float) * places * d);
+  w.piece_ml = off; off += align_up(sizeof(float) * 2 * places);
+  w.total = off;
+  return w;
+}
+void launch_prefix_attention(const PrefixCall& p, int dtype, int d, char* ws, hipStream_t s);
+
 }  // namespace sa

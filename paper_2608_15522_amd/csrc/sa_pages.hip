@@ -1,0 +1,509 @@
+// Pages of keys and values: which page holds which tokens (reserve, fork, free,
+// compact: integers only), and the moves of the rows themselves (write, copy).
+//
+// A cache is described by page_table [B][max_pages] (page numbers, -1 = none),
+// seq_len [B] (tokens of each sequence) and page_ref [n_pages] (table entries that
+// name the page; 0 = free).  Free pages are handed out lowest number first, in the
+// order of the sequences and of their pages, so every result is determined by its
+// inputs alone.
+#include "sa_device.h"
+#include "sa_internal.h"
+
+namespace sa {
+namespace {
+
+constexpr int kScanThreads = 1024;
+constexpr int kScanWaves = kScanThreads / kWave;
+constexpr int kScanEach = 16;                           // pages per thread and step
+constexpr int kScanStep = kScanThreads * kScanEach;     // pages per step
+
+__device__ __forceinline__ int pages_of(long long tokens, int lp) {
+  return static_cast<int>((tokens + (1ll << lp) - 1) >> lp);
+}
+
+// Page flags of one step, kept as the ballots of the wave's 16 loads (64 consecutive
+// pages each, so the loads are coalesced and a page's rank is a count of bits).
+// One workgroup takes 16384 pages a step: 64 bytes in flight a lane.
+struct PageFlags {
+  uint64_t m[kScanEach];
+  template <class F>
+  __device__ __forceinline__ void read(int p0, int n_pages, F flag) {
+    const int lane = threadIdx.x & 63;
+    bool f[kScanEach];
+#pragma unroll
+    for (int j = 0; j < kScanEach; ++j) {
+      const int p = p0 + 64 * j + lane;
+      f[j] = p < n_pages && flag(p);
+    }
+#pragma unroll
+    for (int j = 0; j < kScanEach; ++j) m[j] = __ballot(f[j]);
+  }
+  __device__ __forceinline__ int count() const {
+    int c = 0;
+#pragma unroll
+    for (int j = 0; j < kScanEach; ++j) c += __popcll(m[j]);
+    return c;
+  }
+  // f(page, rank) for each flagged page of the lane; rank counts from `before`.
+  template <class F>
+  __device__ __forceinline__ void each(int p0, int before, F f) const {
+    const int lane = threadIdx.x & 63;
+    const uint64_t below = (1ull << lane) - 1ull;
+#pragma unroll
+    for (int j = 0; j < kScanEach; ++j) {
+      if ((m[j] >> lane) & 1) f(p0 + 64 * j + lane, before + __popcll(m[j] & below));
+      before += __popcll(m[j]);
+    }
+  }
+};
+
+// Sum over the waves of a workgroup-wide step: returns the total, `before` the part
+// of the waves in front of this one.  `slot` alternates so that one barrier is enough.
+__device__ __forceinline__ int step_total(int own, int slot, int (*tot)[kScanWaves], int* before) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  if (lane == 0) tot[slot][wave] = own;
+  __syncthreads();
+  int sum = 0, pre = 0;
+#pragma unroll
+  for (int w = 0; w < kScanWaves; ++w) {
+    const int v = tot[slot][w];
+    if (w < wave) pre += v;
+    sum += v;
+  }
+  *before = pre;
+  return sum;
+}
+
+__device__ __forceinline__ int step_page(int p0) { return p0 + (threadIdx.x >> 6) * 64 * kScanEach; }
+
+// Free pages among the first ones that are needed: exact if fewer than `want`.
+__device__ int count_free(const int32_t* __restrict__ ref, int n_pages, long long want,
+                          int (*tot)[kScanWaves]) {
+  int found = 0, before;
+  for (int p0 = 0, k = 0; p0 < n_pages && found < want; p0 += kScanStep, ++k) {
+    PageFlags f;
+    f.read(step_page(p0), n_pages, [&](int p) { return ref[p] == 0; });
+    found += step_total(f.count(), k & 1, tot, &before);
+  }
+  __syncthreads();
+  return found;
+}
+
+// take(page, rank) for the `want` lowest free pages (there are so many), which get one
+// owner.
+template <class F>
+__device__ void take_free(int32_t* __restrict__ ref, int n_pages, int want,
+                          int (*tot)[kScanWaves], F take) {
+  int base = 0;
+  for (int p0 = 0, k = 0; p0 < n_pages && base < want; p0 += kScanStep, ++k) {
+    PageFlags f;
+    f.read(step_page(p0), n_pages, [&](int p) { return ref[p] == 0; });
+    int before;
+    const int all = step_total(f.count(), k & 1, tot, &before);
+    f.each(step_page(p0), base + before, [&](int p, int rank) {
+      if (rank < want) {
+        take(p, rank);
+        ref[p] = 1;
+      }
+    });
+    base += all;
+  }
+}
+
+// Inclusive sum over the workgroup's threads, in 64 bits.
+__device__ long long scan_threads(long long v, long long* wave_tot, long long* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const long long u = __shfl_up(v, o, 64);
+    if (lane >= o) v += u;
+  }
+  if (lane == 63) wave_tot[wave] = v;
+  __syncthreads();
+  long long sum = 0, pre = 0;
+#pragma unroll
+  for (int w = 0; w < kScanWaves; ++w) {
+    if (w < wave) pre += wave_tot[w];
+    sum += wave_tot[w];
+  }
+  __syncthreads();
+  *total = sum;
+  return v + pre;
+}
+
+// New pages of sequence b: tokens len .. len + n - 1.
+__device__ __forceinline__ int2 reserve_span(const int32_t* __restrict__ seq_len,
+                                             const int32_t* __restrict__ n_new, int b, int lp) {
+  const long long len = max(seq_len[b], 0), n = max(n_new[b], 0);
+  return make_int2(pages_of(len, lp), pages_of(len + n, lp));
+}
+
+// One workgroup: the pages' order is a prefix sum over the sequences, then one over the
+// free pages.  Latency-bound (a few dependent loads and barriers).
+__global__ void __launch_bounds__(kScanThreads)
+pages_reserve_kernel(int32_t* __restrict__ table, int32_t* __restrict__ seq_len,
+                     int32_t* __restrict__ ref, const int32_t* __restrict__ n_new, int B,
+                     int max_pages, int n_pages, int lp, int32_t* __restrict__ missing) {
+  __shared__ int tot[2][kScanWaves];
+  __shared__ long long wave_tot[kScanWaves];
+  __shared__ int ends[kMaxSequences];  // pages of the sequences up to and with b
+  const int tid = threadIdx.x;
+  const int each = ceil_div(B, kScanThreads);
+  const int b0 = min(tid * each, B), b1 = min(b0 + each, B);
+  long long own = 0, over = 0;
+  for (int b = b0; b < b1; ++b) {
+    const int2 s = reserve_span(seq_len, n_new, b, lp);
+    own += s.y - s.x;
+    over += max(s.y - max_pages, 0);
+  }
+  long long total, lacking;
+  long long at = scan_threads(own, wave_tot, &total) - own;
+  scan_threads(over, wave_tot, &lacking);
+  const int found = count_free(ref, n_pages, total, tot);
+  lacking += max(total - found, 0ll);
+  if (tid == 0) missing[0] = static_cast<int32_t>(min(lacking, 0x7fffffffll));
+  if (lacking > 0) return;
+  for (int b = b0; b < b1; ++b) {  // total <= n_pages: 32 bits
+    const int2 s = reserve_span(seq_len, n_new, b, lp);
+    at += s.y - s.x;
+    ends[b] = static_cast<int>(at);
+  }
+  __syncthreads();
+  take_free(ref, n_pages, static_cast<int>(total), tot, [&](int p, int rank) {
+    int lo = 0, hi = B - 1;  // the first b with ends[b] > rank
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (ends[mid] > rank)
+        hi = mid;
+      else
+        lo = mid + 1;
+    }
+    const int2 s = reserve_span(seq_len, n_new, lo, lp);
+    table[static_cast<size_t>(lo) * max_pages + s.y - (ends[lo] - rank)] = p;
+  });
+  __syncthreads();
+  for (int b = b0; b < b1; ++b) seq_len[b] = max(seq_len[b], 0) + max(n_new[b], 0);
+}
+
+// Entries of a fork: src must hold tokens and dst none, so the two sets are disjoint;
+// of several entries with one dst the first able one counts.
+__device__ __forceinline__ bool fork_able(const int32_t* __restrict__ seq_len, int src, int dst,
+                                          int B) {
+  return src >= 0 && src < B && dst >= 0 && dst < B && seq_len[src] > 0 && seq_len[dst] <= 0;
+}
+
+// Pass 1 (one workgroup): which entries count, and a fresh page for each partial last
+// page.  copy_src holds kNoFork for an entry that does not count.
+constexpr int kNoFork = -2;
+__global__ void __launch_bounds__(kScanThreads)
+pages_fork_plan_kernel(const int32_t* __restrict__ table, const int32_t* __restrict__ seq_len,
+                       int32_t* __restrict__ ref, const int32_t* __restrict__ src,
+                       const int32_t* __restrict__ dst, int n, int B, int max_pages, int n_pages,
+                       int lp, int32_t* __restrict__ copy_src, int32_t* __restrict__ copy_dst,
+                       int32_t* __restrict__ missing) {
+  __shared__ int tot[2][kScanWaves];
+  __shared__ long long wave_tot[kScanWaves];
+  __shared__ int first[kMaxSequences];  // first able entry of each dst; then entries by rank
+  const int tid = threadIdx.x;
+  for (int b = tid; b < B; b += kScanThreads) first[b] = 0x7fffffff;
+  __syncthreads();
+  for (int i = tid; i < n; i += kScanThreads)
+    if (fork_able(seq_len, src[i], dst[i], B)) atomicMin(&first[dst[i]], i);
+  __syncthreads();
+  const int each = ceil_div(n, kScanThreads);
+  const int i0 = min(tid * each, n), i1 = min(i0 + each, n);
+  auto counts = [&](int i) {
+    return fork_able(seq_len, src[i], dst[i], B) && first[dst[i]] == i;
+  };
+  auto partial = [&](int i) { return (seq_len[src[i]] & ((1 << lp) - 1)) != 0; };
+  int own = 0;
+  for (int i = i0; i < i1; ++i) own += counts(i) && partial(i);
+  long long total;
+  int rank = static_cast<int>(scan_threads(own, wave_tot, &total)) - own;
+  const int found = count_free(ref, n_pages, total, tot);
+  const int lacking = max(static_cast<int>(total) - found, 0);
+  if (tid == 0) missing[0] = lacking;
+  for (int i = i0; i < i1; ++i) {
+    int last = kNoFork;
+    if (lacking == 0 && counts(i)) {
+      const int full = seq_len[src[i]] >> lp;
+      last = partial(i) && full < max_pages
+                 ? table[static_cast<size_t>(src[i]) * max_pages + full] : -1;
+      if (last < 0 && last != -1) last = -1;  // an entry that is no page: nothing to copy
+    }
+    copy_src[i] = last;
+    copy_dst[i] = -1;
+  }
+  if (lacking > 0) return;
+  __syncthreads();  // every thread is done with `first`
+  // entries by the rank of their fresh page: total <= n <= B
+  int* entry = first;
+  uint64_t mine = 0;  // each <= 16: the thread's entries that need one
+  for (int i = i0; i < i1; ++i)
+    if (copy_src[i] != kNoFork && partial(i)) mine |= 1ull << (i - i0);
+  for (int i = i0; i < i1; ++i)
+    if ((mine >> (i - i0)) & 1) entry[rank++] = i;
+  __syncthreads();
+  take_free(ref, n_pages, static_cast<int>(total), tot,
+            [&](int p, int r) { copy_dst[entry[r]] = p; });
+}
+
+// Pass 2 (one workgroup an entry): dst's row is src's, with the fresh page in the place
+// of the partial last one, and every shared page gets an owner more.
+__global__ void __launch_bounds__(256)
+pages_fork_kernel(int32_t* __restrict__ table, int32_t* __restrict__ seq_len,
+                  int32_t* __restrict__ ref, const int32_t* __restrict__ src,
+                  const int32_t* __restrict__ dst, int max_pages, int n_pages, int lp,
+                  int32_t* __restrict__ copy_src, const int32_t* __restrict__ copy_dst) {
+  const int i = blockIdx.x, tid = threadIdx.x;
+  const int last = copy_src[i], fresh = copy_dst[i];
+  __syncthreads();
+  if (last == kNoFork) {
+    if (tid == 0) copy_src[i] = -1;
+    return;
+  }
+  const int a = src[i], len = seq_len[a], full = len >> lp;
+  const int32_t* from = table + static_cast<size_t>(a) * max_pages;
+  int32_t* to = table + static_cast<size_t>(dst[i]) * max_pages;
+  for (int j = tid; j < max_pages; j += 256) {
+    int p = j == full ? fresh : -1;
+    if (j < full) {
+      p = from[j];
+      if (p >= 0 && p < n_pages) atomicAdd(ref + p, 1);
+    }
+    to[j] = p;
+  }
+  if (tid == 0) seq_len[dst[i]] = len;
+}
+
+// One workgroup an entry; a sequence named twice is freed once, by its first entry.
+__global__ void __launch_bounds__(256)
+pages_free_kernel(int32_t* __restrict__ table, int32_t* __restrict__ seq_len,
+                  int32_t* __restrict__ ref, const int32_t* __restrict__ seqs, int B,
+                  int max_pages, int n_pages, int lp) {
+  const int i = blockIdx.x, tid = threadIdx.x;
+  const int b = seqs[i];
+  bool seen = b < 0 || b >= B;
+  for (int j = tid; j < i && !seen; j += 256) seen = seqs[j] == b;
+  if (__syncthreads_or(seen)) return;
+  const int held = min(pages_of(max(seq_len[b], 0), lp), max_pages);
+  int32_t* row = table + static_cast<size_t>(b) * max_pages;
+  for (int j = tid; j < max_pages; j += 256) {
+    if (j < held) {
+      const int p = row[j];
+      if (p >= 0 && p < n_pages) atomicSub(ref + p, 1);
+    }
+    row[j] = -1;
+  }
+  __syncthreads();  // every thread has read the length
+  if (tid == 0) seq_len[b] = 0;
+}
+
+// Pass 1 (one workgroup): with U pages in use, the k-th used page from number U on
+// moves to the k-th free page below U.
+__global__ void __launch_bounds__(kScanThreads)
+pages_compact_plan_kernel(const int32_t* __restrict__ ref, int n_pages,
+                          int32_t* __restrict__ move_src, int32_t* __restrict__ move_dst,
+                          int32_t* __restrict__ counts) {
+  __shared__ int tot[2][kScanWaves];
+  int used = 0, before;
+  for (int p0 = 0, k = 0; p0 < n_pages; p0 += kScanStep, ++k) {
+    PageFlags f;
+    f.read(step_page(p0), n_pages, [&](int p) { return ref[p] > 0; });
+    used += step_total(f.count(), k & 1, tot, &before);
+  }
+  __syncthreads();
+  int holes = 0, high = 0;
+  for (int p0 = 0, k = 0; p0 < n_pages; p0 += kScanStep, ++k) {
+    // a step may hold both: free pages below `used`, used ones from there on
+    PageFlags f;
+    f.read(step_page(p0), n_pages, [&](int p) { return (ref[p] > 0) == (p >= used); });
+    PageFlags g = f;
+    const int w0 = step_page(p0);
+#pragma unroll
+    for (int j = 0; j < kScanEach; ++j) {
+      const int first = w0 + 64 * j;  // bits of pages below `used`
+      const int n = used - first;
+      const uint64_t low = n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull;
+      f.m[j] &= low;
+      g.m[j] &= ~low;
+    }
+    const int a = step_total(f.count(), 0, tot, &before);
+    f.each(w0, holes + before, [&](int p, int r) { move_dst[r] = p; });
+    holes += a;
+    const int c = step_total(g.count(), 1, tot, &before);
+    g.each(w0, high + before, [&](int p, int r) { move_src[r] = p; });
+    high += c;
+  }
+  for (int r = high + threadIdx.x; r < n_pages / 2; r += kScanThreads)
+    move_src[r] = move_dst[r] = -1;
+  if (threadIdx.x == 0) {
+    counts[0] = used;
+    counts[1] = high;
+  }
+}
+
+// Pass 2: table entries of moved pages (found in the ascending move_src by halving),
+// and the owners' counts.
+__global__ void __launch_bounds__(256)
+pages_compact_kernel(int32_t* __restrict__ table, int32_t* __restrict__ ref, size_t entries,
+                     int n_pages, const int32_t* __restrict__ move_src,
+                     const int32_t* __restrict__ move_dst, const int32_t* __restrict__ counts) {
+  const int used = counts[0], moves = counts[1];
+  const size_t step = static_cast<size_t>(gridDim.x) * 256;
+  for (size_t i = static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x;
+       i < entries || i < static_cast<size_t>(moves); i += step) {
+    if (i < static_cast<size_t>(moves)) {
+      ref[move_dst[i]] = ref[move_src[i]];
+      ref[move_src[i]] = 0;
+    }
+    if (i >= entries) continue;
+    const int p = table[i];
+    if (p < used || p >= n_pages || moves == 0) continue;
+    int lo = 0, hi = moves - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (move_src[mid] >= p)
+        hi = mid;
+      else
+        lo = mid + 1;
+    }
+    if (move_src[lo] == p) table[i] = move_dst[lo];
+  }
+}
+
+// Copies of whole pages within every pool, HBM-bound.  A unit of work is kCopyUnit bytes
+// of one page; a workgroup takes every gridDim.x-th one, 64 list entries looked up at
+// once, so that entries to be skipped (-1: a list filled up to its capacity) cost a
+// lane each and no latency of their own.
+constexpr int kCopyThreads = 256;
+constexpr int kCopyLoads = 4;  // 16-byte loads in flight a thread
+constexpr int kCopyUnit = kCopyThreads * kCopyLoads * 16;
+__global__ void __launch_bounds__(kCopyThreads)
+pages_copy_kernel(char* __restrict__ pools, int n_pools, int n_pages, size_t page_bytes,
+                  const int32_t* __restrict__ src, const int32_t* __restrict__ dst, int n) {
+  const int lane = threadIdx.x & 63;
+  const size_t chunks = (page_bytes + kCopyUnit - 1) / kCopyUnit;
+  const size_t per = chunks * n_pools, units = per * n;
+  for (size_t u0 = blockIdx.x; u0 < units; u0 += 64ull * gridDim.x) {
+    const size_t u = u0 + static_cast<size_t>(lane) * gridDim.x;
+    int from = -1, to = -1;
+    unsigned pool = 0, chunk = 0;
+    if (u < units) {
+      const size_t e = u / per, r = u - e * per;
+      from = src[e];
+      to = dst[e];
+      pool = static_cast<unsigned>(r / chunks);
+      chunk = static_cast<unsigned>(r - pool * chunks);
+    }
+    uint64_t todo = __ballot(from >= 0 && from < n_pages && to >= 0 && to < n_pages);
+    while (todo != 0) {
+      const int l = __ffsll(static_cast<unsigned long long>(todo)) - 1;
+      todo &= todo - 1;
+      const size_t base = static_cast<size_t>(__builtin_amdgcn_readlane(pool, l)) * n_pages;
+      const size_t off = static_cast<size_t>(__builtin_amdgcn_readlane(chunk, l)) * kCopyUnit;
+      const char* a = pools + (base + __builtin_amdgcn_readlane(from, l)) * page_bytes;
+      char* b = pools + (base + __builtin_amdgcn_readlane(to, l)) * page_bytes;
+      u32x4 x[kCopyLoads];
+#pragma unroll
+      for (int k = 0; k < kCopyLoads; ++k) {
+        const size_t at = off + (k * kCopyThreads + threadIdx.x) * 16ull;
+        if (at < page_bytes) x[k] = ldg16_nt(a + at);
+      }
+#pragma unroll
+      for (int k = 0; k < kCopyLoads; ++k) {
+        const size_t at = off + (k * kCopyThreads + threadIdx.x) * 16ull;
+        if (at < page_bytes) stg16(b + at, x[k]);
+      }
+    }
+  }
+}
+
+// Rows of k and v into their pages: one 16-byte piece of both a thread, HBM-bound for
+// many tokens, latency-bound for one (length, table entry, rows: three loads in turn).
+__global__ void __launch_bounds__(256)
+pages_write_kernel(const char* __restrict__ k, const char* __restrict__ v,
+                   char* __restrict__ k_pages, char* __restrict__ v_pages,
+                   const int32_t* __restrict__ table, const int32_t* __restrict__ seq_len,
+                   const int32_t* __restrict__ n_new, int Hkv, int S, int log_cpr,
+                   unsigned rows, int max_pages, int n_pages, int lp) {
+  const size_t pieces = static_cast<size_t>(rows) << log_cpr;
+  const size_t step = static_cast<size_t>(gridDim.x) * 256;
+  for (size_t i = static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x; i < pieces; i += step) {
+    const unsigned row = static_cast<unsigned>(i >> log_cpr);
+    const unsigned bh = row / S, s = row - bh * S;
+    const unsigned b = bh / Hkv, h = bh - b * Hkv;
+    const int n = n_new != nullptr ? min(n_new[b], S) : S;
+    const long long pos = static_cast<long long>(seq_len[b]) - n + s;
+    const long long j = pos >> lp;
+    if (static_cast<int>(s) >= n || pos < 0 || j >= max_pages) continue;
+    const int p = table[static_cast<size_t>(b) * max_pages + j];
+    if (p < 0 || p >= n_pages) continue;
+    const size_t to = ((((static_cast<size_t>(p) * Hkv + h) << lp) + (pos & ((1 << lp) - 1)))
+                       << log_cpr) + (i & ((1u << log_cpr) - 1));
+    const u32x4 a = ldg16_nt(k + 16 * i), c = ldg16_nt(v + 16 * i);
+    stg16(k_pages + 16 * to, a);
+    stg16(v_pages + 16 * to, c);
+  }
+}
+
+inline int log2_of(int x) { return __builtin_ctz(static_cast<unsigned>(x)); }
+
+}  // namespace
+
+void launch_pages_reserve(int32_t* table, int32_t* seq_len, int32_t* ref, const int32_t* n_new,
+                          int B, int max_pages, int n_pages, int page, int32_t* missing,
+                          hipStream_t s) {
+  hipLaunchKernelGGL(pages_reserve_kernel, dim3(1), dim3(kScanThreads), 0, s, table, seq_len, ref,
+                     n_new, B, max_pages, n_pages, log2_of(page), missing);
+}
+
+void launch_pages_fork(int32_t* table, int32_t* seq_len, int32_t* ref, const int32_t* src,
+                       const int32_t* dst, int n, int B, int max_pages, int n_pages, int page,
+                       int32_t* copy_src, int32_t* copy_dst, int32_t* missing, hipStream_t s) {
+  hipLaunchKernelGGL(pages_fork_plan_kernel, dim3(1), dim3(kScanThreads), 0, s, table, seq_len,
+                     ref, src, dst, n, B, max_pages, n_pages, log2_of(page), copy_src, copy_dst,
+                     missing);
+  hipLaunchKernelGGL(pages_fork_kernel, dim3(n), dim3(256), 0, s, table, seq_len, ref, src, dst,
+                     max_pages, n_pages, log2_of(page), copy_src, copy_dst);
+}
+
+void launch_pages_free(int32_t* table, int32_t* seq_len, int32_t* ref, const int32_t* seqs, int n,
+                       int B, int max_pages, int n_pages, int page, hipStream_t s) {
+  hipLaunchKernelGGL(pages_free_kernel, dim3(n), dim3(256), 0, s, table, seq_len, ref, seqs, B,
+                     max_pages, n_pages, log2_of(page));
+}
+
+void launch_pages_compact(int32_t* table, int32_t* ref, int B, int max_pages, int n_pages,
+                          int32_t* move_src, int32_t* move_dst, int32_t* counts, hipStream_t s) {
+  hipLaunchKernelGGL(pages_compact_plan_kernel, dim3(1), dim3(kScanThreads), 0, s, ref, n_pages,
+                     move_src, move_dst, counts);
+  const size_t entries = static_cast<size_t>(B) * max_pages;
+  const size_t most = entries > static_cast<size_t>(n_pages) / 2 ? entries : n_pages / 2 + 1;
+  const size_t wgs = (most + 255) / 256;
+  hipLaunchKernelGGL(pages_compact_kernel, dim3(static_cast<unsigned>(wgs < 2048 ? wgs : 2048)),
+                     dim3(256), 0, s, table, ref, entries, n_pages, move_src, move_dst, counts);
+}
+
+void launch_pages_copy(void* pools, int n_pools, int n_pages, size_t page_bytes,
+                       const int32_t* src, const int32_t* dst, int n, hipStream_t s) {
+  const size_t units = (page_bytes + kCopyUnit - 1) / kCopyUnit * n_pools * n;
+  hipLaunchKernelGGL(pages_copy_kernel, dim3(static_cast<unsigned>(units < 2048 ? units : 2048)),
+                     dim3(kCopyThreads), 0, s, static_cast<char*>(pools), n_pools, n_pages,
+                     page_bytes, src, dst, n);
+}
+
+void launch_pages_write(const void* k, const void* v, void* k_pages, void* v_pages,
+                        const int32_t* table, const int32_t* seq_len, const int32_t* n_new, int B,
+                        int Hkv, int S, int row_bytes, int max_pages, int n_pages, int page,
+                        hipStream_t s) {
+  const unsigned rows = static_cast<unsigned>(B) * Hkv * S;
+  const int log_cpr = log2_of(row_bytes / 16);
+  const size_t wgs = ((static_cast<size_t>(rows) << log_cpr) + 255) / 256;
+  hipLaunchKernelGGL(pages_write_kernel, dim3(static_cast<unsigned>(wgs < 8192 ? wgs : 8192)),
+                     dim3(256), 0, s, static_cast<const char*>(k), static_cast<const char*>(v),
+                     static_cast<char*>(k_pages), static_cast<char*>(v_pages), table, seq_len,
+                     n_new, Hkv, S, log_cpr, rows, max_pages, n_pages, log2_of(page));
+}
+
+}  // namespace sa

@@ -1,0 +1,811 @@
+// Attention of a batch over keys and values kept in pages (sa_prefix_attention): the
+// sequences of a group may share their first pages, whose keys are then read once for
+// all of the group's queries.
+//
+// O = softmax(scale Q K^T) V over the keys of a sequence.  With the keys cut into parts
+// i, each with its running max m_i (log2 units), sum l_i = sum 2^(x - m_i) and
+// unnormalised row O_i = sum 2^(x - m_i) v, the whole is
+//   M = max m_i,  O = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i,
+// so the shared keys can be taken against the queries of all sequences of the group at
+// once and the sequences' own keys one sequence at a time.
+//
+// Segments.  Per key head: the shared keys of each group against the rows of all its
+// sequences (kShared; only where a sequence has few rows), then each sequence's other
+// keys against its own rows.  The rows of (sequence, key head) are its Hq / Hkv heads
+// times S queries, which lie one behind the other in Q.  A segment is row tiles times
+// 64-key tiles; all of them, head by head, laid end to end are the call's units of work,
+// cut into equal runs, one per workgroup slot of the chip.  The lengths are read on the
+// device, so a captured call follows them; every workgroup finds its run by the same
+// prefix sums over the segments.  A row tile that runs share leaves partial rows, which
+// prefix_combine_kernel joins in key order, so results do not depend on timing.
+#include <float.h>
+
+#include "sa_device.h"
+#include "sa_internal.h"
+
+namespace sa {
+namespace {
+
+typedef __attribute__((address_space(3))) uint16_t lds_u16_t;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4_t;
+
+constexpr int kTile = 64;         // keys per unit of work
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / kWave;
+constexpr int kSegs = kMaxAttendSegs;
+
+// The running max is raised when a score exceeds it by 2^8, as in the other attention
+// kernels: weights stay below 2^8, exact after the division by the row sum.
+constexpr float kRescaleSlack = 8.0f;
+constexpr float kSlackWeight = 1.f / 256.f;  // 2^-kRescaleSlack
+
+struct Args {
+  const void* q;
+  const void* kp;
+  const void* vp;
+  void* o;
+  float* lse;
+  const int32_t* table;
+  const int32_t* seq_len;
+  const int32_t* shared_len;  // NULL: nothing shared
+  const int32_t* q_len;       // NULL: S queries each
+  int B, G, N;                // sequences, groups (0: no shared segments), sequences a group
+  int Hkv, R, S, RS;          // key heads, query heads a key head, queries, R * S
+  int n_pages, lp, max_pages, causal;
+  int TRp, TRo;               // rows of a row tile: shared segments, own segments
+  int TR;                     // the larger of the two: rows of a partial row tile's place
+  int run_min;                // least units of a run
+  Log2Scale c;
+  long long* sched;           // [kSegs + 2] prefix sums, run
+  int* sched_sh;              // [G]
+  float* full;                // [2][B * Hq * S][D] partial rows of whole row tiles
+  float2* full_ml;            // [2][B * Hq * S]
+  float* piece;               // [2 slots][TR][D] partial rows of shared row tiles
+  float2* piece_ml;           // [2 slots][TR]
+};
+
+// Units that a row tile costs besides its 64-key tiles (its Q rows, its epilogue).
+constexpr int kRowCost = 1;
+
+__device__ __forceinline__ int seq_tokens(const Args& a, int b) {
+  const long long cap = static_cast<long long>(a.max_pages) << a.lp;
+  const int len = a.seq_len[b];
+  return len < 0 ? 0 : static_cast<int>(len < cap ? len : cap);
+}
+__device__ __forceinline__ int seq_queries(const Args& a, int b) {
+  return a.q_len != nullptr ? min(max(a.q_len[b], 0), a.S) : a.S;
+}
+
+// Prefix sums of the segments' units of one head, and the shared tokens of each group:
+// whole pages, at most what every sequence with a key has and (causal) what its first
+// query sees.
+struct Schedule {
+  long long off[kSegs + 1];
+  int sh[kSegs / 2];
+  long long wave_tot[kWaves];
+};
+
+__device__ void build_schedule(const Args& a, Schedule& s) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (a.G > 0) {
+    for (int g = tid; g < a.G; g += kThreads) s.sh[g] = 0x7fffffff;
+    __syncthreads();
+    for (int b = tid; b < a.B; b += kThreads) {
+      const int len = seq_tokens(a, b);
+      if (len > 0)
+        atomicMin(&s.sh[b / a.N], a.causal ? max(min(len - seq_queries(a, b) + 1, len), 0) : len);
+    }
+    __syncthreads();
+    for (int g = tid; g < a.G; g += kThreads) {
+      // no sequence of the group has a key: nothing to share
+      const int v = s.sh[g] == 0x7fffffff ? 0 : min(s.sh[g], max(a.shared_len[g], 0));
+      s.sh[g] = v >> a.lp << a.lp;
+    }
+    __syncthreads();
+  }
+  const int n = a.G + a.B, each = ceil_div(n, kThreads);
+  const int i0 = min(tid * each, n), i1 = min(i0 + each, n);
+  auto units = [&](int i) -> long long {
+    if (i < a.G) {
+      const int nk = ceil_div(s.sh[i], kTile);
+      return nk == 0 ? 0 : static_cast<long long>(ceil_div(a.N * a.RS, a.TRp)) * (nk + kRowCost);
+    }
+    const int b = i - a.G, len = seq_tokens(a, b);
+    const int own = a.G > 0 ? max(len - s.sh[b / a.N], 0) : len;
+    return static_cast<long long>(ceil_div(a.RS, a.TRo)) * (ceil_div(own, kTile) + kRowCost);
+  };
+  long long sum = 0;
+  for (int i = i0; i < i1; ++i) sum += units(i);
+  long long incl = sum;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const long long u = __shfl_up(incl, o, 64);
+    if (lane >= o) incl += u;
+  }
+  if (lane == 63) s.wave_tot[wave] = incl;
+  __syncthreads();
+  long long at = incl - sum;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w)
+    if (w < wave) at += s.wave_tot[w];
+  for (int i = i0; i < i1; ++i) {
+    s.off[i] = at;
+    at += units(i);
+  }
+  if (i1 == n && i0 < n) s.off[n] = at;
+  __syncthreads();
+}
+
+// What one workgroup does at a time: 64-key tiles [t0, t1) of a row tile of a segment.
+struct Job {
+  int h;            // key head
+  int b0;           // kShared: first sequence of the group; else the sequence
+  int rows;         // rows of the segment
+  int row0;         // first row of the tile
+  int pos0, pos1;   // key positions of the segment
+  const int32_t* pages;  // table row that they are read through
+  int t0, t1;
+  bool shared;
+  bool whole;       // all tiles of the row tile
+  int piece;        // place of the partial rows if not
+};
+
+// Row rho of a segment: sequence, row within (sequence, key head), whether it exists.
+struct Row {
+  int b, in;
+  bool real;
+};
+__device__ __forceinline__ Row row_of(const Args& a, const Job& j, int rho) {
+  Row r;
+  const bool inside = rho < j.rows;
+  rho = inside ? rho : j.rows - 1;
+  const int k = j.shared ? rho / a.RS : 0;
+  r.b = j.b0 + k;
+  r.in = rho - k * a.RS;
+  r.real = inside && r.in % a.S < seq_queries(a, r.b);
+  return r;
+}
+__device__ __forceinline__ size_t row_index(const Args& a, int h, const Row& r) {
+  return (static_cast<size_t>(r.b) * a.Hkv + h) * a.RS + r.in;
+}
+
+// 64 table entries ahead of a sweep over ascending positions, one a lane, the next 64
+// on their way: a page number is then a lane read.
+struct PageCursor {
+  const int32_t* pages;
+  int max_pages, n_pages, lp;
+  int base, cur, next;
+  __device__ __forceinline__ int load(int i) const {
+    i += threadIdx.x & 63;
+    return i < max_pages ? pages[i] : -1;
+  }
+  __device__ __forceinline__ void start(const Args& a, const int32_t* p, int pos) {
+    pages = p;
+    max_pages = a.max_pages;
+    n_pages = a.n_pages;
+    lp = a.lp;
+    base = __builtin_amdgcn_readfirstlane(pos >> lp);
+    cur = load(base);
+    next = load(base + 64);
+  }
+  // Row of the pool (in tokens of one head, page 0 for an entry that is no page) that
+  // holds position pos, pos being at most 64 pages behind the last one asked for.
+  __device__ __forceinline__ size_t row(int pos, int h, int Hkv) {
+    int i = __builtin_amdgcn_readfirstlane(pos >> lp) - base;
+    if (i >= 64) {
+      base += 64;
+      i -= 64;
+      cur = next;
+      next = load(base + 64);
+    }
+    int p = __builtin_amdgcn_readlane(cur, i);
+    p = p >= 0 && p < n_pages ? p : 0;
+    return (((static_cast<size_t>(p) * Hkv + h) << lp) + (pos & ((1 << lp) - 1)));
+  }
+};
+
+// Whether a table entry of positions [pos, end) is no page: its keys are left out.
+__device__ __forceinline__ bool bad_pages(const Args& a, const int32_t* pages, int pos, int end) {
+  bool bad = false;
+  const int last = ceil_div(end, 1 << a.lp);
+  for (int i = (pos >> a.lp) + (threadIdx.x & 63); i < last; i += 64) {
+    const int p = pages[i];
+    bad = bad || p < 0 || p >= a.n_pages;
+  }
+  return __any(bad);
+}
+__device__ __forceinline__ bool bad_page(const Args& a, const int32_t* pages, int pos) {
+  const int i = pos >> a.lp;
+  if (i >= a.max_pages) return true;
+  const int p = pages[i];
+  return p < 0 || p >= a.n_pages;
+}
+
+__device__ __forceinline__ float max_halves(float x) {
+  const auto pr = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x),
+                                                   false, false);
+  return fmaxf(x, fmaxf(__uint_as_float(pr[0]), __uint_as_float(pr[1])));
+}
+__device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xC07F); }  // lgkmcnt(0)
+
+// Last key position that a row sees, plus one.
+__device__ __forceinline__ int row_end(const Args& a, const Job& j, const Row& r) {
+  if (!a.causal || j.shared) return j.pos1;
+  const int last = seq_tokens(a, r.b) - seq_queries(a, r.b) + r.in % a.S;
+  return min(j.pos1, last + 1);
+}
+
+// ---- rows out ---------------------------------------------------------------------------
+// Four channels of a row and its (m, l), m in log2 units: to O and lse if the row tile is
+// whole and nothing is to be joined to it, else to the row's place among the partial rows.
+template <int D, typename T>
+__device__ __forceinline__ void store_row(const Args& a, size_t at, int c4, f32x4 num, float m,
+                                          float l) {
+  const float inv = l != 0.f ? 1.f / l : 0.f;  // a row without a key is zeros
+  if constexpr (sizeof(T) == 2)
+    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.o) + at * D + 4 * c4) =
+        u32x2{pack_bf16x2(num[0] * inv, num[1] * inv), pack_bf16x2(num[2] * inv, num[3] * inv)};
+  else
+    *reinterpret_cast<f32x4*>(static_cast<float*>(a.o) + at * D + 4 * c4) =
+        f32x4{num[0] * inv, num[1] * inv, num[2] * inv, num[3] * inv};
+  if (a.lse != nullptr && c4 == 0)
+    a.lse[at] = l == 0.f ? -INFINITY
+                         : static_cast<float>(static_cast<double>(m) * 0.6931471805599453 +
+                                              static_cast<double>(logf(l)));
+}
+template <int D, typename T>
+__device__ __forceinline__ void put_row(const Args& a, const Job& j, int jr, int c4, f32x4 num,
+                                        float m, float l) {
+  const Row r = row_of(a, j, j.row0 + jr);
+  if (j.whole && a.G == 0) {
+    if (r.real) store_row<D, T>(a, row_index(a, j.h, r), c4, num, m, l);
+    return;
+  }
+  size_t at = static_cast<size_t>(j.piece) * a.TR + jr;
+  if (j.whole)
+    at = (j.shared ? 0 : static_cast<size_t>(a.B) * a.Hkv * a.RS) + row_index(a, j.h, r);
+  *reinterpret_cast<f32x4*>((j.whole ? a.full : a.piece) + at * D + 4 * c4) = num;
+  if (c4 == 0) (j.whole ? a.full_ml : a.piece_ml)[at] = make_float2(m, l);
+}
+
+// Joins the waves' partial rows of a row tile, in wave order.  A wave's rows lie in its
+// own LDS buffers (W bytes each), slot c4 of row r at join_slot(r, c4).
+constexpr int kJoinRows = 32;
+template <int D>
+__device__ __forceinline__ int join_slot(int r, int c4) {
+  return r * D * 4 + ((c4 ^ r) & (D / 4 - 1)) * 16;
+}
+template <int D, int W, typename T>
+__device__ __forceinline__ void join_waves(const Args& a, const Job& j, int rows,
+                                           const char* lds_all, const float2* lds_ml) {
+  __syncthreads();
+  constexpr int TPR = D / 4;
+  for (int u = threadIdx.x; u < rows * TPR; u += kThreads) {
+    const int jr = u / TPR, c4 = u % TPR;
+    float M = -FLT_MAX, den = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w)
+      if (lds_ml[w * kJoinRows + jr].y != 0.f) M = fmaxf(M, lds_ml[w * kJoinRows + jr].x);
+    f32x4 num = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float2 ml = lds_ml[w * kJoinRows + jr];
+      const float f = ml.y != 0.f ? fast_exp2(ml.x - M) : 0.f;
+      const f32x4 x = *reinterpret_cast<const f32x4*>(lds_all + w * W + join_slot<D>(jr, c4));
+      den = fmaf(f, ml.y, den);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) num[e] = fmaf(f, x[e], num[e]);
+    }
+    put_row<D, T>(a, j, jr, c4, num, M, den);
+  }
+  __syncthreads();  // the buffers may be filled again
+}
+
+// ---- bf16, few rows ---------------------------------------------------------------------
+// 32 rows to a workgroup; its waves take 32-key pieces in turn, each through 16 KB (d = 128)
+// of LDS of its own, so the loop has no barrier, and join their rows at the end.  Bound by
+// HBM: each key row is used for 32 rows at most.  A wave has one buffer for K and one for
+// V, refilled by LDS DMA as soon as it is used up: K of the next piece is on its way during
+// the softmax and P V, V during the next piece's Q K^T.
+constexpr int kPiece = 32;
+template <int D>
+__device__ void attend_few(const Args& a, const Job& j, char* lds_all, float2* lds_ml) {
+  constexpr int KC = D / 16, DT = D / 32, NI = kPiece * D * 2 / 1024;
+  constexpr int BUF = kPiece * D * 2;  // bytes
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, n = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  char* lds = lds_all + wave * 2 * BUF;
+  const uint32_t lds_k = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)(lds_void_t*)lds);
+  const uint32_t lds_v = lds_k + BUF;
+
+  const Row row = row_of(a, j, j.row0 + n);
+  const uint16_t* q = static_cast<const uint16_t*>(a.q);
+  u32x4 qf[KC];
+#pragma unroll
+  for (int kc = 0; kc < KC; ++kc)
+    qf[kc] = row.real ? ldg16(q + row_index(a, j.h, row) * D + 16 * kc + 8 * g)
+                      : u32x4{0u, 0u, 0u, 0u};
+  const int end = row_end(a, j, row);
+  const int run0 = j.pos0 + kTile * j.t0, run1 = min(j.pos1, j.pos0 + kTile * j.t1);
+  const bool bad = bad_pages(a, j.pages, run0, run1);
+
+  // DMA: 1 KB = 16 rows of one 32-channel plane; lane l's source is the 16-byte slot that
+  // the swizzle keeps at slot l % 4 of row l / 4.
+  const uint32_t voff = static_cast<uint32_t>((lane >> 2) * (D * 2) +
+                                              16 * ((lane & 3) ^ plane_swz(lane >> 2)));
+  const int k_off0 = n * 64 + 16 * ((0 + g) ^ plane_swz(n));
+  const int k_off1 = n * 64 + 16 * ((2 + g) ^ plane_swz(n));
+  const int grp = lane >> 4, gi = lane & 15;
+  const int tr_key = 4 * (grp >> 1) + (gi >> 2);
+  const int tr_byte = 32 * (grp & 1) + 8 * (gi & 3);
+  const int v_off0 = tr_key * 64 + 16 * ((tr_byte >> 4) ^ plane_swz(tr_key)) + (tr_byte & 15);
+  const int v_off1 = (8 + tr_key) * 64 + 16 * ((tr_byte >> 4) ^ plane_swz(8 + tr_key)) +
+                     (tr_byte & 15);
+
+  const int first = run0 + kPiece * wave;
+  PageCursor cur;
+  cur.start(a, j.pages, min(first, max(run1 - 1, 0)));
+  size_t off[2];  // byte offsets of the piece's two 16-row groups, the same in K and V
+  auto look = [&](int pos) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) off[u] = cur.row(pos + 16 * u, j.h, a.Hkv) * (D * 2);
+  };
+  auto issue = [&](const void* pool, uint32_t to) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+      lds_dma16(static_cast<const char*>(pool) + off[i & 1], voff + 64 * (i >> 1),
+                to + (i >> 1) * 2048 + (i & 1) * 1024);
+  };
+
+  f32x16 acc[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) acc[dt] = zero16();
+  float m = -FLT_MAX, lsum = 0.f;
+  const float c = a.c.hi + a.c.lo;
+  if (first < run1) {
+    look(first);
+    issue(a.kp, lds_k);
+    issue(a.vp, lds_v);
+  }
+  for (int pos = first; pos < run1; pos += kPiece * kWaves) {
+    const bool more = pos + kPiece * kWaves < run1;
+    const bool masked = bad || pos + kPiece > run1 || (a.causal && !j.shared);
+    wait_vm<NI>();  // K; V's copies are behind it
+    __builtin_amdgcn_sched_barrier(0);
+    f32x16 s = zero16();
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc) {
+      const u32x4 ka = *reinterpret_cast<const u32x4*>(lds + (kc >> 1) * 2048 +
+                                                       ((kc & 1) ? k_off1 : k_off0));
+      s = mfma32x32x16(ka, qf[kc], s);
+    }
+    wait_lds();  // the reads of K are done
+    __builtin_amdgcn_sched_barrier(0);
+    if (more) {
+      look(pos + kPiece * kWaves);
+      issue(a.kp, lds_k);
+    }
+    bool none[2] = {false, false};  // the piece's 16-key groups without a page
+    if (masked) {
+      if (bad) {
+        none[0] = bad_page(a, j.pages, pos);
+        none[1] = bad_page(a, j.pages, pos + 16);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int key = crow(i, g);
+        if (pos + key >= end || none[key >> 4]) s[i] = -INFINITY;
+      }
+    }
+    float mx = s[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+    mx = max_halves(mx) * c;
+    if (__any(mx > m + kRescaleSlack)) {
+      const float m_new = fmaxf(m, mx);
+      const float alpha = fast_exp2(m - m_new);
+      m = m_new;
+      lsum *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[dt][i] *= alpha;
+    }
+    // the row sum in fp32, the weights of P V rounded to bf16 (its operand type): half a
+    // step of 2^-8 each, averaged over the keys
+    uint32_t pb[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float p0 = fast_exp2(fmaf(s[2 * i], c, -m));
+      const float p1 = fast_exp2(fmaf(s[2 * i + 1], c, -m));
+      lsum += p0 + p1;
+      pb[i] = pack_bf16x2(p0, p1);
+    }
+    if (more)
+      wait_vm<NI>();  // V; the next K's copies are behind it
+    else
+      wait_dma();
+    __builtin_amdgcn_sched_barrier(0);
+    if (masked) {
+      // rows of V that no row of the workgroup sees may hold anything, NaN too: zeros
+      const int rr = lane >> 1;  // a row's halves of every plane
+      const bool gone = pos + rr >= run1 || (rr < 16 ? none[0] : none[1]);
+      if (gone) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          char* z = lds + BUF + dt * 2048 + rr * 64 + (lane & 1) * 32;
+          *reinterpret_cast<u32x4*>(z) = u32x4{0u, 0u, 0u, 0u};
+          *reinterpret_cast<u32x4*>(z + 16) = u32x4{0u, 0u, 0u, 0u};
+        }
+      }
+      wait_lds();
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    const lds_u16_t* Vb = (const lds_u16_t*)(lds + BUF);
+#pragma unroll
+    for (int mm = 0; mm < 2; ++mm) {
+      const u32x4 b = {pb[4 * mm], pb[4 * mm + 1], pb[4 * mm + 2], pb[4 * mm + 3]};
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const lds_u16_t* base = Vb + (dt * 2048 + mm * 1024) / 2;
+        const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (lds_s16x4_t*)(base + v_off0 / 2)));
+        const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (lds_s16x4_t*)(base + v_off1 / 2)));
+        acc[dt] = mfma32x32x16(u32x4{lo.x, lo.y, hi.x, hi.y}, b, acc[dt]);
+      }
+    }
+    wait_lds();  // the reads of V are done
+    __builtin_amdgcn_sched_barrier(0);
+    if (more) issue(a.vp, lds_v);
+  }
+
+  // the wave's rows in its own buffers, 16-byte slots swizzled by row
+  const int rows = min(32, j.rows - j.row0);
+  const float ltot = lsum + swap_halves(lsum);
+  if (n < rows) {
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int rg = 0; rg < 4; ++rg)
+        *reinterpret_cast<f32x4*>(lds + join_slot<D>(n, 8 * dt + 2 * rg + g)) =
+            f32x4{acc[dt][4 * rg], acc[dt][4 * rg + 1], acc[dt][4 * rg + 2], acc[dt][4 * rg + 3]};
+    if (g == 0) lds_ml[wave * kJoinRows + n] = make_float2(m, ltot);
+  }
+  join_waves<D, 2 * BUF, uint16_t>(a, j, rows, lds_all, lds_ml);
+}
+
+// ---- fp32 -------------------------------------------------------------------------------
+// 16 rows to a workgroup; its waves take 16-key pieces in turn: K through LDS buffers of
+// their own (RowTile16), V in registers, both one piece ahead, products in fp32
+// (v_mfma_f32_16x16x4_f32):
+//   S^T = K Q^T    lane (n, gk) = (l % 16, l / 16) holds channels 16i + 4gk + e of Q[n]
+//                  and K[n]; the result leaves it with keys 4gk .. 4gk + 3 of query n;
+//   O^T += V^T P^T with k slot gk of step r standing for key 4gk + r, and row i of channel
+//                  tile (dq, e) for channel 64dq + 4i + e.
+// Weights are taken down by 2^-8, the slack of the running max, so that none exceeds 1.
+constexpr int kF32Keys = 16;
+template <int D>
+__device__ void attend_f32(const Args& a, const Job& j, char* lds_all, float2* lds_ml) {
+  constexpr int KI = D / 16, DQ = D / 64;
+  using KTile = RowTile16<D>;
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, gk = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  char* lds = lds_all + wave * 2 * KTile::kBytes;
+  const Row row = row_of(a, j, j.row0 + n);
+  const float* q = static_cast<const float*>(a.q);
+  f32x4 qf[KI];
+#pragma unroll
+  for (int i = 0; i < KI; ++i)
+    qf[i] = row.real ? ldg_f32x4(q + row_index(a, j.h, row) * D + 16 * i + 4 * gk)
+                     : f32x4{0.f, 0.f, 0.f, 0.f};
+  const int end = row_end(a, j, row);
+  const int run0 = j.pos0 + kTile * j.t0, run1 = min(j.pos1, j.pos0 + kTile * j.t1);
+  const bool bad = bad_pages(a, j.pages, run0, run1);
+  const int first = run0 + kF32Keys * wave;
+  PageCursor cur;
+  cur.start(a, j.pages, min(first, max(run1 - 1, 0)));
+  KTile kt;
+  kt.init(lds, lane);
+  struct Piece {
+    f32x4 v[4][DQ];
+  };
+  auto load = [&](int pos, int buf, Piece& x) {
+    const size_t at = cur.row(pos, j.h, a.Hkv) * D;
+    kt.copy(static_cast<const float*>(a.kp) + at, 0, kF32Keys, buf);
+    const float* v = static_cast<const float*>(a.vp) + at;
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int dq = 0; dq < DQ; ++dq) x.v[s][dq] = ldg_f32x4(v + (4 * gk + s) * D + 4 * n + 64 * dq);
+  };
+  f32x4 acc[DQ][4];
+#pragma unroll
+  for (int dq = 0; dq < DQ; ++dq)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[dq][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -FLT_MAX, lsum = 0.f;
+  constexpr int STEP = kF32Keys * kWaves;
+  auto step = [&](int pos, int buf, Piece& x, Piece& nx) {
+    wait_dma();
+    __builtin_amdgcn_sched_barrier(0);
+    f32x4 kf[KI];
+    kt.read(buf, kf);
+    if (pos + STEP < run1) load(pos + STEP, buf ^ 1, nx);
+    __builtin_amdgcn_sched_barrier(0);
+    f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < KI; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; e += 2) {
+        s0 = mfma16x16x4_f32(kf[i][e], qf[i][e], s0);
+        s1 = mfma16x16x4_f32(kf[i][e + 1], qf[i][e + 1], s1);
+      }
+    float s[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[e] = s0[e] + s1[e];
+    if (bad || pos + kF32Keys > run1 || (a.causal && !j.shared)) {
+      const bool none = bad && bad_page(a, j.pages, pos);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int key = pos + 4 * gk + e;
+        if (key >= end || none) s[e] = -INFINITY;
+        // rows of V that no row of the workgroup sees may hold anything, NaN too
+        if (key >= run1 || none)
+#pragma unroll
+          for (int dq = 0; dq < DQ; ++dq) x.v[e][dq] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+    }
+    const float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])) * a.c.hi;
+    if (__any(mx > m + kRescaleSlack)) {
+      float m_new = fmaxf(m, mx);
+      m_new = fmaxf(m_new, __shfl_xor(m_new, 16, 64));
+      m_new = fmaxf(m_new, __shfl_xor(m_new, 32, 64));
+      const float alpha = fast_exp2(m - m_new);
+      m = m_new;
+      lsum *= alpha;
+#pragma unroll
+      for (int dq = 0; dq < DQ; ++dq)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[dq][e] *= alpha;
+    }
+    float p[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) p[e] = kSlackWeight * fast_exp2(log2_score(s[e], a.c, m));
+    lsum += (p[0] + p[1]) + (p[2] + p[3]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int dq = 0; dq < DQ; ++dq)
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+          acc[dq][w] = mfma16x16x4_f32(x.v[e][dq][w], p[e], acc[dq][w]);
+  };
+  Piece xa, xb;
+  if (first < run1) {
+    load(first, 0, xa);
+    int pos = first;
+    for (; pos + STEP < run1; pos += 2 * STEP) {
+      step(pos, 0, xa, xb);
+      step(pos + STEP, 1, xb, xa);
+    }
+    if (pos < run1) step(pos, 0, xa, xb);
+  }
+  lsum += __shfl_xor(lsum, 16, 64);
+  lsum += __shfl_xor(lsum, 32, 64);
+  const int rows = min(16, j.rows - j.row0);
+  wait_lds();
+  if (n < rows) {
+    // acc[dq][e][s] is channel 64dq + 16gk + 4s + e of query n
+#pragma unroll
+    for (int dq = 0; dq < DQ; ++dq)
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+        *reinterpret_cast<f32x4*>(lds + join_slot<D>(n, 16 * dq + 4 * gk + s)) =
+            f32x4{acc[dq][0][s], acc[dq][1][s], acc[dq][2][s], acc[dq][3][s]};
+    // 2^-8 goes back into the reference, exactly
+    if (gk == 0) lds_ml[wave * kJoinRows + n] = make_float2(m + kRescaleSlack, lsum);
+  }
+  join_waves<D, 2 * KTile::kBytes, float>(a, j, rows, lds_all, lds_ml);
+}
+
+// Bytes of LDS that the waves' buffers take: 16 KB a wave at d = 128 for either type.
+template <int D>
+constexpr int attend_lds() {
+  return kWaves * 128 * D;
+}
+
+// ---- the runs ---------------------------------------------------------------------------
+// The units of a run, and the run of a unit.  Runs of one slot each; equal but for the
+// last ones of a small call.
+__device__ __forceinline__ long long run_units(const Args& a, long long total, int slots) {
+  const long long run = (total + slots - 1) / slots;
+  return run < a.run_min ? a.run_min : run;
+}
+
+template <int D, typename T>
+__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
+prefix_attention_kernel(const Args a) {
+  __shared__ __attribute__((aligned(1024))) char lds[attend_lds<D>()];
+  __shared__ float2 lds_ml[kWaves * 32];
+  __shared__ Schedule s;
+  build_schedule(a, s);
+  const int n = a.G + a.B;
+  const long long per_head = s.off[n], total = per_head * a.Hkv;
+  const long long run = run_units(a, total, gridDim.x);
+  if (blockIdx.x == 0 && a.sched != nullptr) {  // for the kernel that joins the rows
+    for (int i = threadIdx.x; i <= n; i += kThreads) a.sched[i] = s.off[i];
+    for (int i = threadIdx.x; i < a.G; i += kThreads) a.sched_sh[i] = s.sh[i];
+  }
+  // consecutive runs on one XCD, so that row tiles of a head share their keys in its L2
+  const int per_xcd = gridDim.x >> 3;
+  const int slot = (gridDim.x & 7) != 0 ? blockIdx.x : (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+  long long u = slot * run;
+  const long long stop = u + run < total ? u + run : total;
+  while (u < stop) {
+    const int h = static_cast<int>(u / per_head);
+    const long long in = u - h * per_head;
+    int lo = 0, hi = n - 1;  // the last segment that starts at or before `in` and is not empty
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (s.off[mid] <= in)
+        lo = mid;
+      else
+        hi = mid - 1;
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    Job j;
+    j.h = __builtin_amdgcn_readfirstlane(h);
+    j.shared = lo < a.G;
+    int tr;
+    if (j.shared) {
+      j.b0 = lo * a.N;
+      j.rows = a.N * a.RS;
+      j.pos0 = 0;
+      j.pos1 = s.sh[lo];
+      tr = a.TRp;
+      int rep = j.b0;  // the group's first sequence with a key
+      while (rep + 1 < j.b0 + a.N && seq_tokens(a, rep) == 0) ++rep;
+      j.pages = a.table + static_cast<size_t>(rep) * a.max_pages;
+    } else {
+      j.b0 = lo - a.G;
+      j.rows = a.RS;
+      const int len = seq_tokens(a, j.b0);
+      j.pos0 = a.G > 0 ? min(s.sh[j.b0 / a.N], len) : 0;
+      j.pos1 = len;
+      tr = a.TRo;
+      j.pages = a.table + static_cast<size_t>(j.b0) * a.max_pages;
+    }
+    j.pos0 = __builtin_amdgcn_readfirstlane(j.pos0);
+    j.pos1 = __builtin_amdgcn_readfirstlane(j.pos1);
+    const int per = ceil_div(j.pos1 - j.pos0, kTile) + kRowCost;
+    const long long x = in - s.off[lo];
+    const int rt = __builtin_amdgcn_readfirstlane(static_cast<int>(x / per));
+    const int k0 = __builtin_amdgcn_readfirstlane(
+        static_cast<int>(x - static_cast<long long>(rt) * per));
+    const int take = __builtin_amdgcn_readfirstlane(
+        static_cast<int>(stop - u < per - k0 ? stop - u : per - k0));
+    j.row0 = rt * tr;
+    j.t0 = max(k0 - kRowCost, 0);
+    j.t1 = max(k0 + take - kRowCost, 0);
+    j.whole = k0 == 0 && take == per;
+    j.piece = 2 * slot + (k0 > 0 ? 0 : 1);
+    if constexpr (sizeof(T) == 2)
+      attend_few<D>(a, j, lds, lds_ml);
+    else
+      attend_f32<D>(a, j, lds, lds_ml);
+    u += take;
+  }
+}
+
+// Joins the partial rows of every row: those of the shared keys, then those of its own, in
+// key order.  4 channels of a row a thread.
+template <int D, typename T>
+__global__ void __launch_bounds__(256)
+prefix_combine_kernel(const Args a, int slots) {
+  constexpr int TPR = D / 4;
+  const size_t gid =
+      (static_cast<size_t>(blockIdx.z) * gridDim.x + blockIdx.x) * 256 + threadIdx.x;
+  const size_t row = gid / TPR, rows = static_cast<size_t>(a.B) * a.Hkv * a.RS;
+  if (row >= rows) return;
+  const int c4 = static_cast<int>(gid % TPR);
+  const size_t bh = row / a.RS;
+  const int in = static_cast<int>(row - bh * a.RS);
+  const int b = static_cast<int>(bh / a.Hkv), h = static_cast<int>(bh - static_cast<size_t>(b) * a.Hkv);
+  if (in % a.S >= seq_queries(a, b)) return;
+  const int n = a.G + a.B, len = seq_tokens(a, b);
+  const long long per_head = a.sched[n], total = per_head * a.Hkv;
+  const long long run = run_units(a, total, slots);
+  float M = -FLT_MAX, den = 0.f;
+  f32x4 num = {0.f, 0.f, 0.f, 0.f};
+  auto add = [&](const float* o, float2 ml) {
+    if (ml.y == 0.f) return;
+    const float m = fmaxf(M, ml.x), fa = fast_exp2(M - m), fb = fast_exp2(ml.x - m);
+    const f32x4 x = ldg_f32x4(o + 4 * c4);
+    M = m;
+    den = fmaf(fb, ml.y, fa * den);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) num[e] = fmaf(fb, x[e], fa * num[e]);
+  };
+  auto segment = [&](int seg, int keys, int rho, int tr, size_t full_at) {
+    const int per = ceil_div(keys, kTile) + kRowCost;
+    const long long u0 = h * per_head + a.sched[seg] + static_cast<long long>(rho / tr) * per;
+    const int first = static_cast<int>(u0 / run), last = static_cast<int>((u0 + per - 1) / run);
+    if (first == last) {
+      if (a.G > 0) add(a.full + full_at * D, a.full_ml[full_at]);
+      return a.G > 0;
+    }
+    for (int s = first; s <= last; ++s) {
+      const size_t at = static_cast<size_t>(2 * s + (s == first ? 1 : 0)) * a.TR + rho % tr;
+      // a run that starts with the row tile's first unit holds it from its beginning
+      add(a.piece + at * D, a.piece_ml[at]);
+    }
+    return true;
+  };
+  if (len > 0) {
+    const int g = a.G > 0 ? b / a.N : 0;
+    const int sh = a.G > 0 ? a.sched_sh[g] : 0;
+    if (sh > 0) segment(g, sh, (b - g * a.N) * a.RS + in, a.TRp, row);
+    if (!segment(a.G + b, len - sh, in, a.TRo, rows + row)) return;  // written already
+  } else if (a.G == 0) {
+    return;
+  }
+  store_row<D, T>(a, row, c4, num, M, den);
+}
+
+}  // namespace
+
+void launch_prefix_attention(const PrefixCall& p, int dtype, int d, char* ws, hipStream_t s) {
+  const PrefixWs w = prefix_ws_layout(p.B, p.Hq, p.Hkv, p.S, d, dtype, p.n_groups);
+  Args a{};
+  a.q = p.q;
+  a.kp = p.k_pages;
+  a.vp = p.v_pages;
+  a.o = p.o;
+  a.lse = p.lse;
+  a.table = p.page_table;
+  a.seq_len = p.seq_len;
+  a.shared_len = p.shared_len;
+  a.q_len = p.q_len;
+  a.B = p.B;
+  a.G = w.groups;
+  a.N = w.groups > 0 ? p.B / w.groups : 0;
+  a.Hkv = p.Hkv;
+  a.R = p.Hq / p.Hkv;
+  a.S = p.S;
+  a.RS = a.R * p.S;
+  a.n_pages = p.n_pages;
+  a.lp = __builtin_ctz(static_cast<unsigned>(p.page));
+  a.max_pages = p.max_pages;
+  a.causal = p.causal;
+  a.TRp = w.shared_rows;
+  a.TRo = w.own_rows;
+  a.TR = w.piece_rows;
+  a.run_min = 4;
+  a.c = log2_scale(p.scale);
+  a.sched = reinterpret_cast<long long*>(ws + w.sched);
+  a.sched_sh = reinterpret_cast<int*>(ws + w.sched_sh);
+  a.full = reinterpret_cast<float*>(ws + w.full);
+  a.full_ml = reinterpret_cast<float2*>(ws + w.full_ml);
+  a.piece = reinterpret_cast<float*>(ws + w.piece);
+  a.piece_ml = reinterpret_cast<float2*>(ws + w.piece_ml);
+  const size_t threads = static_cast<size_t>(p.B) * p.Hq * p.S * (d / 4);
+  const dim3 cgrid = wide_grid(static_cast<long>((threads + 255) / 256));
+#define SA_PREFIX(D, T)                                                                       \
+  hipLaunchKernelGGL((prefix_attention_kernel<D, T>), dim3(kPrefixSlots), dim3(kThreads), 0, s, \
+                     a);                                                                      \
+  hipLaunchKernelGGL((prefix_combine_kernel<D, T>), cgrid, dim3(256), 0, s, a, kPrefixSlots)
+  if (dtype == 0 && d == 128) {
+    SA_PREFIX(128, uint16_t);
+  } else if (dtype == 0) {
+    SA_PREFIX(64, uint16_t);
+  } else if (d == 128) {
+    SA_PREFIX(128, float);
+  } else {
+    SA_PREFIX(64, float);
+  }
+#undef SA_PREFIX
+}
+
+}  // namespace sa

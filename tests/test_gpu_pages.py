@@ -1,0 +1,308 @@
+"""Pages of a cache on the GPU against the plain lists of oracle.pages: every integer
+equal, every copied value equal bit for bit."""
+import random
+
+import pytest
+import torch
+
+import paper_2608_15522_amd as sa
+from oracle import pages
+
+pytestmark = pytest.mark.gpu
+I32 = dict(dtype=torch.int32, device="cuda")
+
+
+def ints(v):
+    return torch.tensor(v, **I32)
+
+
+def filled(seed, B, n_pages, width, page, longest, used=0.6):
+    """Lists of a cache with about `used` of its pages taken, some shared."""
+    rng = random.Random(seed)
+    table, lens, ref = [[-1] * width for _ in range(B)], [0] * B, [0] * n_pages
+    order = list(range(n_pages))
+    rng.shuffle(order)
+    budget = int(used * n_pages)
+    for b in range(B):
+        n = min(rng.randrange(0, longest + 1), width * page, budget * page)
+        for j in range(-(-n // page)):
+            table[b][j] = order.pop()
+            ref[table[b][j]] += 1
+        budget -= -(-n // page)
+        lens[b] = n
+    return table, lens, ref
+
+
+def on_gpu(lists):
+    return [ints(x) for x in lists]
+
+
+def same(got, want):
+    for g, w in zip(got, want):
+        assert g.tolist() == (w if isinstance(w, list) else [w])
+
+
+SIZES = [  # B, n_pages, width, page, longest
+    (1, 1, 1, 16, 16), (3, 7, 4, 16, 60), (9, 100, 12, 32, 300), (64, 4096, 40, 64, 2000),
+    (5, 40000, 3000, 16, 40000), (1000, 33000, 33, 16, 500), (16384, 20000, 2, 128, 200),
+]
+
+
+@pytest.mark.parametrize("B,n_pages,width,page,longest", SIZES)
+def test_reserve(B, n_pages, width, page, longest):
+    print(f"case reserve B={B} n_pages={n_pages} page={page}", flush=True)
+    for seed, most in ((1, 1), (2, 2 * page + 3), (3, page)):
+        table, lens, ref = filled(seed, B, n_pages, width, page, longest)
+        rng = random.Random(seed + 10)
+        n_new = [rng.randrange(-1, most + 1) for _ in range(B)]
+        n_new = [min(m, width * page - n) for m, n in zip(n_new, lens)]
+        t, n, r = on_gpu((table, lens, ref))
+        missing = sa.sa_pages_reserve(t, n, r, ints(n_new), page)
+        want = pages.reserve(table, lens, ref, n_new, page)
+        same((t, n, r, missing), want)
+
+
+def test_reserve_is_all_or_nothing():
+    for lists, n_new, page in [
+            (([[2, -1, -1], [-1, -1, -1]], [3, 0], [0, 0, 1, 0]), [50, 20], 16),   # free pages
+            (([[2, -1, -1], [-1, -1, -1]], [3, 0], [0, 0, 1, 0]), [1, 49], 16),    # table row
+            (([[-1]], [0], [1] * 20000), [16], 16),                                # none free
+            (([[-1] * 4], [-5], [0] * 3), [33, ], 16),                             # negative length
+            (([[-1] * 4], [0], [0] * 3), [2 ** 31 - 1], 128)]:
+        t, n, r = on_gpu(lists)
+        missing = sa.sa_pages_reserve(t, n, r, ints(n_new), page)
+        same((t, n, r, missing), pages.reserve(*lists, n_new, page))
+
+
+@pytest.mark.parametrize("B,n_pages,width,page,longest", SIZES)
+def test_fork(B, n_pages, width, page, longest):
+    print(f"case fork B={B} n_pages={n_pages} page={page}", flush=True)
+    for seed in range(3):
+        table, lens, ref = filled(seed, B, n_pages, width, page, longest, 0.5)
+        rng = random.Random(seed)
+        gone = rng.sample(range(B), B // 2)
+        table, lens, ref = pages.free(table, lens, ref, gone, page)
+        k = max(1, B // 2)
+        # sequences outside the table, with no tokens, in use, and dst named twice, too
+        src = [rng.randrange(-1, B + 1) for _ in range(k)]
+        dst = [rng.choice(gone) if gone and rng.random() < 0.8 else rng.randrange(-1, B + 1)
+               for _ in range(k)]
+        t, n, r = on_gpu((table, lens, ref))
+        a, b, missing = sa.sa_pages_fork(t, n, r, ints(src), ints(dst), page)
+        same((t, n, r, a, b, missing), pages.fork(table, lens, ref, src, dst, page))
+
+
+def test_fork_without_room_changes_nothing():
+    lists = ([[0, 1], [2, -1], [-1, -1], [-1, -1]], [20, 16, 0, 0], [1, 1, 1])
+    for src, dst in (([0, 1], [2, 3]), ([1, 1], [2, 3])):  # the second needs no fresh page
+        t, n, r = on_gpu(lists)
+        a, b, missing = sa.sa_pages_fork(t, n, r, ints(src), ints(dst), 16)
+        same((t, n, r, a, b, missing), pages.fork(*lists, src, dst, 16))
+
+
+@pytest.mark.parametrize("B,n_pages,width,page,longest", SIZES)
+def test_free(B, n_pages, width, page, longest):
+    print(f"case free B={B} n_pages={n_pages} page={page}", flush=True)
+    for seed in range(2):
+        table, lens, ref = filled(seed, B, n_pages, width, page, longest)
+        rng = random.Random(seed)
+        seqs = [rng.randrange(-2, B + 2) for _ in range(rng.randrange(1, min(2 * B, 16384) + 1))]
+        t, n, r = on_gpu((table, lens, ref))
+        sa.sa_pages_free(t, n, r, ints(seqs), page)
+        same((t, n, r), pages.free(table, lens, ref, seqs, page))
+
+
+@pytest.mark.parametrize("B,n_pages,width,page,longest", SIZES)
+@pytest.mark.parametrize("used", [0.0, 0.1, 0.5, 0.9])
+def test_compact(B, n_pages, width, page, longest, used):
+    print(f"case compact B={B} n_pages={n_pages} used={used}", flush=True)
+    table, lens, ref = filled(7, B, n_pages, width, page, longest, used)
+    t, r = on_gpu((table, ref))
+    a, b, c = sa.sa_pages_compact(t, r)
+    same((t, r, a, b, c), pages.compact(table, ref))
+
+
+@pytest.mark.parametrize("dtype,n_pools,n_pages,shape", [
+    (torch.bfloat16, 1, 5, (1, 16, 64)), (torch.bfloat16, 3, 40, (8, 64, 128)),
+    (torch.float32, 2, 70, (5, 32, 64)), (torch.uint8, 4, 300, (16,)),
+    (torch.bfloat16, 2, 9, (24, 128, 128))])
+def test_copy(dtype, n_pools, n_pages, shape):
+    print(f"case copy pools={n_pools} pages={n_pages} shape={shape}", flush=True)
+    g = torch.Generator(device="cuda").manual_seed(n_pages)
+    pools = (torch.rand(n_pools, n_pages, *shape, device="cuda", generator=g) * 200).to(dtype)
+    rng = random.Random(n_pages)
+    order = rng.sample(range(n_pages), n_pages)
+    dst = order[:n_pages // 2]
+    src = [rng.choice(order[n_pages // 2:]) for _ in dst]  # one source, several copies
+    src, dst = src + [-1, 0, n_pages, -7, 1], dst + [0, -1, 1, -7, n_pages]
+    src[0:0], dst[0:0] = [-1] * 70, [-1] * 70
+    want = pools.clone()
+    for a, b in zip(src, dst):
+        if 0 <= a < n_pages and 0 <= b < n_pages:
+            want[:, b] = pools[:, a]
+    sa.sa_pages_copy(pools, ints(src), ints(dst))
+    assert torch.equal(pools, want)
+    sa.sa_pages_copy(pools, ints([]), ints([]))
+    assert torch.equal(pools, want)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("B,Hkv,S,d,page,longest", [
+    (1, 1, 1, 64, 16, 0), (3, 2, 1, 64, 16, 40), (5, 3, 7, 128, 32, 100), (2, 24, 130, 128, 128, 300),
+    (70, 4, 1, 128, 64, 500), (2, 1, 1000, 64, 16, 33)])
+def test_write(dtype, B, Hkv, S, d, page, longest):
+    print(f"case write B={B} Hkv={Hkv} S={S} d={d} page={page}", flush=True)
+    width = -(-(longest + S) // page) + 1
+    n_pages = B * width + 3
+    table, lens, ref = filled(5, B, n_pages, width, page, longest)
+    for ragged in (False, True):
+        rng = random.Random(B + S)
+        n_new = [rng.randrange(0, S + 1) if ragged else S for _ in range(B)]
+        t2, n2, _, lack = pages.reserve(table, lens, ref, n_new, page)
+        assert lack == 0
+        g = torch.Generator(device="cuda").manual_seed(S)
+        k, v = (torch.randn(B, Hkv, S, d, device="cuda", generator=g).to(dtype) for _ in range(2))
+        kp, vp = (torch.randn(n_pages, Hkv, page, d, device="cuda", generator=g).to(dtype)
+                  for _ in range(2))
+        wk, wv = kp.clone(), vp.clone()
+        for b in range(B):
+            for s in range(n_new[b]):
+                pos = n2[b] - n_new[b] + s
+                wk[t2[b][pos // page], :, pos % page] = k[b, :, s]
+                wv[t2[b][pos // page], :, pos % page] = v[b, :, s]
+        sa.sa_pages_write(k, v, kp, vp, ints(t2), ints(n2), n_new=ints(n_new) if ragged else None)
+        assert torch.equal(kp, wk) and torch.equal(vp, wv)
+
+
+def test_write_skips_tokens_without_a_page():
+    g = torch.Generator(device="cuda").manual_seed(1)
+    k, v = (torch.randn(2, 1, 40, 64, device="cuda", generator=g) for _ in range(2))
+    kp, vp = torch.zeros(4, 1, 16, 64, device="cuda"), torch.zeros(4, 1, 16, 64, device="cuda")
+    # sequence 0: 40 rows for 24 tokens (the first 16 lie before token 0), one page missing;
+    # sequence 1: behind the table row
+    sa.sa_pages_write(k, v, kp, vp, ints([[2, 9], [0, 1]]), ints([24, 60]))
+    want = torch.zeros_like(kp)
+    want[2, 0] = k[0, 0, 16:32]
+    want[1, 0, 4:] = k[1, 0, :12]
+    assert torch.equal(kp, want)
+    want[2, 0] = v[0, 0, 16:32]
+    want[1, 0, 4:] = v[1, 0, :12]
+    assert torch.equal(vp, want)
+
+
+def test_offsets_past_32_bits():
+    """Pools of over 4 GiB: the last pages are written, copied and read."""
+    Hkv, page, d = 16, 128, 128
+    n_pages = 9000  # 512 KiB a page and matrix
+    kp = torch.empty(n_pages, Hkv, page, d, dtype=torch.bfloat16, device="cuda")
+    vp = torch.empty_like(kp)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    k, v = (torch.randn(1, Hkv, 200, d, device="cuda", generator=g).bfloat16() for _ in range(2))
+    table = ints([[n_pages - 1, n_pages - 3]])
+    sa.sa_pages_write(k, v, kp, vp, table, ints([200]))
+    assert torch.equal(kp[n_pages - 1], k[0, :, :128]) and torch.equal(vp[n_pages - 3, :, :72],
+                                                                      v[0, :, 128:])
+    sa.sa_pages_copy(kp.unsqueeze(0), ints([n_pages - 1]), ints([n_pages - 2]))
+    assert torch.equal(kp[n_pages - 2], k[0, :, :128])
+
+
+def test_a_history_of_calls_keeps_cache_and_lists_together():
+    """Steps, forks, frees and compactions in turn: the tokens that each sequence reads
+    through its table are always those that were written for it."""
+    B, Hkv, d, page, width, n_pages, layers = 6, 2, 64, 16, 12, 48, 2
+    rng = random.Random(11)
+    kv = torch.zeros(layers, 2, n_pages, Hkv, page, d, device="cuda")
+    t, n, r = ints([[-1] * width] * B), ints([0] * B), ints([0] * n_pages)
+    tokens = [[] for _ in range(B)]  # the value written for each token
+    count = 0
+    for step in range(40):
+        what = rng.randrange(5) if step else 0
+        if what <= 1:
+            m = [rng.randrange(0, 20) for _ in range(B)]
+            missing = sa.sa_pages_reserve(t, n, r, ints(m), page)
+            if missing.item() == 0:
+                x = torch.zeros(B, Hkv, 20, d, device="cuda")
+                for b in range(B):
+                    for s in range(m[b]):
+                        count += 1
+                        x[b, :, s] = count
+                        tokens[b].append(count)
+                for layer in range(layers):
+                    sa.sa_pages_write(x, -x, kv[layer, 0], kv[layer, 1], t, n, n_new=ints(m))
+        elif what == 2:
+            a, b = rng.sample(range(B), 2)
+            src, dst, missing = sa.sa_pages_fork(t, n, r, ints([a]), ints([b]), page)
+            sa.sa_pages_copy(kv.view(2 * layers, n_pages, Hkv, page, d), src, dst)
+            if missing.item() == 0 and tokens[a] and not tokens[b]:
+                tokens[b] = list(tokens[a])
+        elif what == 3:
+            b = rng.randrange(B)
+            sa.sa_pages_free(t, n, r, ints([b]), page)
+            tokens[b] = []
+        else:
+            src, dst, counts = sa.sa_pages_compact(t, r)
+            sa.sa_pages_copy(kv.view(2 * layers, n_pages, Hkv, page, d), src, dst)
+            assert counts[0].item() == (r > 0).sum().item()
+            assert not (r[counts[0].item():] > 0).any()
+        assert n.tolist() == [len(x) for x in tokens]
+        for b in range(B):
+            ids = t[b, :-(-len(tokens[b]) // page)].long()
+            for sign, pool in ((1, kv[0, 0]), (-1, kv[layers - 1, 1])):
+                got = pool[ids].transpose(1, 2).reshape(-1, Hkv, d)[:len(tokens[b])]
+                want = torch.tensor(tokens[b], device="cuda").float() * sign
+                assert (got == want[:, None, None]).all(), (step, b)
+
+
+def test_captured_calls_follow_the_lists():
+    """Reserve, write, fork, copy and compact in one graph, replayed over changed lists
+    with eager work in between: every replay gives what eager calls give."""
+    B, Hkv, d, page, width, n_pages = 4, 2, 64, 16, 8, 30
+    kp, vp = (torch.zeros(n_pages, Hkv, page, d, device="cuda") for _ in range(2))
+    x = torch.zeros(B, Hkv, 5, d, device="cuda")
+    t, n, r, new = ints([[-1] * width] * B), ints([0] * B), ints([0] * n_pages), ints([0] * B)
+    src, dst = ints([0, 0]), ints([3, 3])
+    buf = dict(copy_src=ints([0, 0]), copy_dst=ints([0, 0]), missing=ints([0]))
+    miss, mv = ints([0]), [ints([0] * (n_pages // 2)) for _ in range(2)]
+    counts = ints([0, 0])
+
+    def calls():
+        sa.sa_pages_reserve(t, n, r, new, page, missing=miss)
+        sa.sa_pages_write(x, x, kp, vp, t, n, n_new=new)
+        sa.sa_pages_free(t, n, r, dst, page)
+        sa.sa_pages_fork(t, n, r, src, dst, page, **buf)
+        for p in (kp, vp):
+            sa.sa_pages_copy(p.unsqueeze(0), buf["copy_src"], buf["copy_dst"])
+        sa.sa_pages_compact(t, r, move_src=mv[0], move_dst=mv[1], counts=counts)
+        for p in (kp, vp):
+            sa.sa_pages_copy(p.unsqueeze(0), *mv)
+
+    state = [kp, vp, t, n, r, buf["copy_src"], buf["copy_dst"], buf["missing"], miss, *mv, counts]
+
+    def start():
+        for z, fill in zip(state, [0, 0, -1, 0, 0] + [0] * 7):
+            z.fill_(fill)
+
+    start()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        calls()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    results = []
+    for replay in (False, True):
+        start()
+        seen = []
+        for step in range(5):
+            new.copy_(ints([(step + b) % 6 for b in range(B)]))
+            x.fill_(step + 1)
+            graph.replay() if replay else calls()
+            torch.cuda.synchronize()
+            seen.append([z.clone() for z in state])
+            torch.randn(1000, device="cuda").sum().item()
+        results.append(seen)
+    for a, b in zip(*results):
+        assert all(torch.equal(p, q) for p, q in zip(a, b))
+    assert results[0][-1][3].tolist()[0] > 0
