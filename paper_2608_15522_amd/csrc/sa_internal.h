@@ -323,7 +323,11 @@ inline PrefixWs prefix_ws_layout(int B, int Hq, int Hkv, int S, int d, int dtype
   PrefixWs w{};
   const long long RS = static_cast<long long>(Hq / Hkv) * S;
   w.groups = n_groups > 0 && B > n_groups && RS < 128 ? n_groups : 0;
-  w.shared_rows = w.own_rows = w.piece_rows = dtype == 0 ? 32 : 16;
+  // bf16: 128 rows a workgroup from 33 on (32 a wave), else 32, its waves at other keys
+  const long long per = w.groups > 0 ? B / w.groups : 1;
+  w.shared_rows = dtype != 0 ? 16 : RS * per > 32 ? 128 : 32;
+  w.own_rows = dtype != 0 ? 16 : RS > 32 ? 128 : 32;
+  w.piece_rows = w.groups > 0 ? w.shared_rows : w.own_rows;
   const size_t rows = static_cast<size_t>(B) * Hq * S;
   size_t off = 0;
   w.sched = off;    off += align_up(sizeof(long long) * (kMaxAttendSegs + 1));

@@ -77,6 +77,12 @@ __device__ __forceinline__ int seq_queries(const Args& a, int b) {
   return a.q_len != nullptr ? min(max(a.q_len[b], 0), a.S) : a.S;
 }
 
+__device__ __forceinline__ long long uniform(long long x) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x));
+  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x >> 32));
+  return static_cast<long long>((static_cast<uint64_t>(hi) << 32) | lo);
+}
+
 // Prefix sums of the segments' units of one head, and the shared tokens of each group:
 // whole pages, at most what every sequence with a key has and (causal) what its first
 // query sees.
@@ -236,6 +242,12 @@ __device__ __forceinline__ int row_end(const Args& a, const Job& j, const Row& r
   return min(j.pos1, last + 1);
 }
 
+__device__ __forceinline__ float natural_lse(float m, float l) {
+  return l == 0.f ? -INFINITY
+                  : static_cast<float>(static_cast<double>(m) * 0.6931471805599453 +
+                                       static_cast<double>(logf(l)));
+}
+
 // ---- rows out ---------------------------------------------------------------------------
 // Four channels of a row and its (m, l), m in log2 units: to O and lse if the row tile is
 // whole and nothing is to be joined to it, else to the row's place among the partial rows.
@@ -249,10 +261,7 @@ __device__ __forceinline__ void store_row(const Args& a, size_t at, int c4, f32x
   else
     *reinterpret_cast<f32x4*>(static_cast<float*>(a.o) + at * D + 4 * c4) =
         f32x4{num[0] * inv, num[1] * inv, num[2] * inv, num[3] * inv};
-  if (a.lse != nullptr && c4 == 0)
-    a.lse[at] = l == 0.f ? -INFINITY
-                         : static_cast<float>(static_cast<double>(m) * 0.6931471805599453 +
-                                              static_cast<double>(logf(l)));
+  if (a.lse != nullptr && c4 == 0) a.lse[at] = natural_lse(m, l);
 }
 template <int D, typename T>
 __device__ __forceinline__ void put_row(const Args& a, const Job& j, int jr, int c4, f32x4 num,
@@ -476,6 +485,362 @@ __device__ void attend_few(const Args& a, const Job& j, char* lds_all, float2* l
   join_waves<D, 2 * BUF, uint16_t>(a, j, rows, lds_all, lds_ml);
 }
 
+// ---- bf16, many rows --------------------------------------------------------------------
+// 128 rows to a workgroup, 32 a wave; 64-key tiles of K and V go through double-buffered
+// LDS that the waves share, by LDS DMA: wave w copies the tile's 16-key group w, which lies
+// in one page.  Bound by the matrix cores.  The products, the softmax and the order of the
+// steady-state loop are those of the block-sparse kernel (sa_attn.hip): S(t+1) = K Q^T runs
+// under the exponentials of tile t, the row max of S(t+1) under P(t) V.  K is copied two
+// tiles ahead, V one.
+constexpr int kManyRows = 128;
+template <int D>
+__device__ void attend_many(const Args& a, const Job& j, char* lds) {
+  constexpr int KC = D / 16, DT = D / 32;
+  constexpr int NI = D / 32;                 // DMA instructions a wave and tile
+  constexpr int TILE = kTile * D * 2;        // bytes of a tile of K or V
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, n = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+  // the lane's row: found again where it is needed, since the loop needs every register
+  auto my_row = [&]() { return row_of(a, j, j.row0 + 32 * wave + n); };
+  u32x4 qf[KC];
+  {
+    const Row row = my_row();
+    const uint16_t* q = static_cast<const uint16_t*>(a.q) + row_index(a, j.h, row) * D + 8 * g;
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc)
+      qf[kc] = row.real ? ldg16(q + 16 * kc) : u32x4{0u, 0u, 0u, 0u};
+  }
+  const int run0 = j.pos0 + kTile * j.t0, run1 = min(j.pos1, j.pos0 + kTile * j.t1);
+  int most = run1, least = run1;       // the furthest and the nearest end of the tile's rows
+  if (a.causal && !j.shared) {
+    const int last = min(j.row0 + kManyRows, j.rows) - 1;
+    const bool one = j.row0 / a.S == last / a.S;  // all of one head: consecutive queries
+    const int nq = seq_queries(a, j.b0), q0 = seq_tokens(a, j.b0) - nq + 1;
+    most = min(run1, q0 + min(one ? last % a.S : a.S - 1, nq - 1));
+    least = min(run1, q0 + (one ? j.row0 % a.S : 0));
+  }
+  const bool bad = bad_pages(a, j.pages, run0, run1);
+  const int T = most > run0 ? ceil_div(most - run0, kTile) : 0;
+  // leading tiles that every row sees whole
+  const int T_full = bad || least <= run0 ? 0 : min((least - run0) / kTile, T);
+
+  // DMA: 1 KB = 16 rows of one 32-channel plane; lane l's source is the 16-byte slot that
+  // the swizzle keeps at slot l % 4 of row l / 4
+  const uint32_t voff = static_cast<uint32_t>((lane >> 2) * (D * 2) +
+                                              16 * ((lane & 3) ^ plane_swz(lane >> 2)));
+  const int k_off0 = n * 64 + 16 * ((0 + g) ^ plane_swz(n));
+  const int k_off1 = n * 64 + 16 * ((2 + g) ^ plane_swz(n));
+  const int grp = lane >> 4, gi = lane & 15;
+  const int tr_key = 4 * (grp >> 1) + (gi >> 2);
+  const int tr_byte = 32 * (grp & 1) + 8 * (gi & 3);
+  const int v_off0 = tr_key * 64 + 16 * ((tr_byte >> 4) ^ plane_swz(tr_key)) + (tr_byte & 15);
+  const int v_off1 = (8 + tr_key) * 64 + 16 * ((tr_byte >> 4) ^ plane_swz(8 + tr_key)) +
+                     (tr_byte & 15);
+
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)(lds_void_t*)lds);
+  // byte addresses of the wave's group in the buffers of tile t
+  auto kdst = [&](int t) { return lds0 + (t & 1) * TILE + wave * 1024; };
+  auto vdst = [&](int t) { return lds0 + (2 + (t & 1)) * TILE + wave * 1024; };
+  auto kbuf = [&](int t) -> const char* { return lds + (t & 1) * TILE; };
+  auto vbuf = [&](int t) -> char* { return lds + (2 + (t & 1)) * TILE; };
+  const char* kp = static_cast<const char*>(a.kp);
+  const char* vp = static_cast<const char*>(a.vp);
+  PageCursor cur;
+  cur.start(a, j.pages, run0 + 16 * wave);
+  // byte offset of the wave's group of tile t, the same in K and V
+  auto look = [&](int t) { return cur.row(run0 + kTile * t + 16 * wave, j.h, a.Hkv) * (D * 2); };
+
+  auto qk = [&](int t, f32x16& s0, f32x16& s1) {
+    const char* Kb = kbuf(t);
+    s0 = zero16();
+    s1 = zero16();
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc) {
+      const int off = (kc & 1) ? k_off1 : k_off0;
+      const u32x4 a0 = *reinterpret_cast<const u32x4*>(Kb + (kc >> 1) * 4096 + off);
+      const u32x4 a1 = *reinterpret_cast<const u32x4*>(Kb + (kc >> 1) * 4096 + 2048 + off);
+      s0 = mfma32x32x16(a0, qf[kc], s0);
+      s1 = mfma32x32x16(a1, qf[kc], s1);
+    }
+  };
+  auto none = [&](int t, int group) {  // a 16-key group without a page
+    return bad && bad_page(a, j.pages, run0 + kTile * t + 16 * group);
+  };
+  auto mask = [&](int t, f32x16& s0, f32x16& s1) {
+    const int left = row_end(a, j, my_row()) - (run0 + kTile * t);
+    bool gone[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) gone[u] = none(t, u);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int key = crow(i, g);
+      if (key >= left || gone[(8 * (i >> 2)) >> 4]) s0[i] = -INFINITY;
+      if (32 + key >= left || gone[2 + ((8 * (i >> 2)) >> 4)]) s1[i] = -INFINITY;
+    }
+  };
+  auto tile_max = [&](const f32x16& s0, const f32x16& s1) {
+    float mx = s0[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s0[i]);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s1[i]);
+    return mx;
+  };
+
+  f32x16 acc[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) acc[dt] = zero16();
+  float m = -FLT_MAX, lsum = 0.f;
+  const float c = a.c.hi + a.c.lo;
+  f32x16 sc0 = zero16(), sc1 = zero16(), sn_0, sn_1;
+  float mx_cur = -INFINITY;
+  size_t off1 = 0;  // of the next tile
+  if (T > 0) {
+    const size_t off0 = look(0);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      lds_dma16(kp + off0 + 64 * i, voff, kdst(0) + i * 4096);
+      lds_dma16(vp + off0 + 64 * i, voff, vdst(0) + i * 4096);
+    }
+    off1 = off0;
+    if (T > 1) {
+      off1 = look(1);
+#pragma unroll
+      for (int i = 0; i < NI; ++i) lds_dma16(kp + off1 + 64 * i, voff, kdst(1) + i * 4096);
+    }
+    wait_dma();
+    __syncthreads();
+    qk(0, sc0, sc1);
+    if (T_full < 1) mask(0, sc0, sc1);
+    mx_cur = tile_max(sc0, sc1);
+    wait_lds();
+    __syncthreads();  // every wave has read K(0) before iteration 0 refills its buffer
+  }
+  auto rescale = [&]() {
+    const float mx = max_halves(mx_cur) * c;
+    if (__any(mx > m + kRescaleSlack)) {
+      const float m_new = fmaxf(m, mx);
+      const float alpha = fast_exp2(m - m_new);
+      m = m_new;
+      lsum *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[dt][i] *= alpha;
+    }
+  };
+  auto vread = [&](const lds_u16_t* Vb, int jj) {
+    const lds_u16_t* base = Vb + ((jj % DT) * 4096 + (jj / DT) * 1024) / 2;
+    const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (lds_s16x4_t*)(base + v_off0 / 2)));
+    const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (lds_s16x4_t*)(base + v_off1 / 2)));
+    return u32x4{lo.x, lo.y, hi.x, hi.y};
+  };
+  // Any tile t: P(t), S(t+1) with its mask, P(t) V(t).  Past the last tile its copies are
+  // repeated into the free buffers.
+  auto iteration = [&](int t) {
+    const size_t off2 = t + 2 < T ? look(t + 2) : off1;
+    if (t >= T_full) {
+      // rows of V that no row of the workgroup sees may hold anything, NaN too: zeros
+      const int rr = 16 * wave + (lane >> 2);
+      if (run0 + kTile * t + rr >= most || none(t, wave)) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+          *reinterpret_cast<u32x4*>(vbuf(t) + i * 4096 + rr * 64 + (lane & 3) * 16) =
+              u32x4{0u, 0u, 0u, 0u};
+      }
+      wait_lds();
+    }
+    __syncthreads();
+    rescale();
+    f32x16 sn0, sn1;
+    qk(t + 1, sn0, sn1);  // on stale data in the last iteration, and then not used
+    if (t + 1 >= T_full && t + 1 < T) mask(t + 1, sn0, sn1);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      lds_dma16(kp + off2 + 64 * i, voff, kdst(t) + i * 4096);
+      lds_dma16(vp + off1 + 64 * i, voff, vdst(t + 1) + i * 4096);
+    }
+    uint32_t pb[16];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float p0 = fast_exp2(fmaf(sc0[2 * i], c, -m));
+      const float p1 = fast_exp2(fmaf(sc0[2 * i + 1], c, -m));
+      const float p2 = fast_exp2(fmaf(sc1[2 * i], c, -m));
+      const float p3 = fast_exp2(fmaf(sc1[2 * i + 1], c, -m));
+      lsum += (p0 + p1) + (p2 + p3);
+      pb[i] = pack_bf16x2(p0, p1);
+      pb[8 + i] = pack_bf16x2(p2, p3);
+    }
+    const lds_u16_t* Vb = (const lds_u16_t*)vbuf(t);
+#pragma unroll
+    for (int jj = 0; jj < 4 * DT; ++jj) {
+      const int mm = jj / DT;
+      const u32x4 b = {pb[4 * mm], pb[4 * mm + 1], pb[4 * mm + 2], pb[4 * mm + 3]};
+      acc[jj % DT] = mfma32x32x16(vread(Vb, jj), b, acc[jj % DT]);
+    }
+    mx_cur = tile_max(sn0, sn1);
+    sc0 = sn0;
+    sc1 = sn1;
+    off1 = off2;
+    wait_dma();
+    __syncthreads();
+  };
+  // Steady state: tiles t and t + 1 need no mask.  The issue order is fixed by scheduling
+  // barriers so that every MFMA is followed by a share of the VALU work: in the Q K^T phase
+  // one bf16 pair of P(t) per MFMA, in three stages a step apart (FMAs, exponentials,
+  // packing); in the P V phase the row max of S(t+1).  Operand reads run two MFMAs ahead,
+  // and the copies are spread over the Q K^T phase.
+  auto main_iter = [&](int t, f32x16& c0, f32x16& c1, f32x16& n0, f32x16& n1) {
+    const size_t off2 = t + 2 < T ? look(t + 2) : off1;
+    const char* kbase = kp + off2;
+    const char* vbase = vp + off1;
+    off1 = off2;
+    rescale();
+    const char* Kb = kbuf(t + 1);
+    const lds_u16_t* Vb = (const lds_u16_t*)vbuf(t);
+    const uint32_t kd = kdst(t), vd = vdst(t + 1);
+    auto kread = [&](int kc, u32x4* dst) {
+      const int off = (kc & 1) ? k_off1 : k_off0;
+      dst[0] = *reinterpret_cast<const u32x4*>(Kb + (kc >> 1) * 4096 + off);
+      dst[1] = *reinterpret_cast<const u32x4*>(Kb + (kc >> 1) * 4096 + 2048 + off);
+    };
+    __builtin_amdgcn_s_setprio(1);
+    constexpr int NA = 2 * KC;          // MFMAs
+    constexpr int PPA = 16 / NA;        // bf16 pairs of P per MFMA
+    u32x4 ka[3][2];
+    uint32_t pb[16];
+    kread(0, ka[0]);
+    kread(1, ka[1]);
+    n0 = zero16();
+    n1 = zero16();
+    float fx[2][PPA][2], ex[2][PPA][2];
+    auto stage_fma = [&](int st) {
+#pragma unroll
+      for (int u = 0; u < PPA; ++u) {
+        const int pk = st * PPA + u;
+        const f32x16& src = pk < 8 ? c0 : c1;
+        const int e = 2 * (pk & 7);
+        fx[st & 1][u][0] = fmaf(src[e], c, -m);
+        fx[st & 1][u][1] = fmaf(src[e + 1], c, -m);
+      }
+    };
+    auto stage_exp = [&](int st) {
+#pragma unroll
+      for (int u = 0; u < PPA; ++u) {
+        ex[st & 1][u][0] = fast_exp2(fx[st & 1][u][0]);
+        ex[st & 1][u][1] = fast_exp2(fx[st & 1][u][1]);
+        lsum += ex[st & 1][u][0] + ex[st & 1][u][1];
+      }
+    };
+    auto stage_pack = [&](int st) {
+#pragma unroll
+      for (int u = 0; u < PPA; ++u)
+        pb[st * PPA + u] = pack_bf16x2(ex[st & 1][u][0], ex[st & 1][u][1]);
+    };
+    stage_fma(0);
+#pragma unroll
+    for (int st = 0; st < NA; ++st) {
+      const int kc = st >> 1;
+      if ((st & 1) == 0 && kc + 2 < KC) kread(kc + 2, ka[(kc + 2) % 3]);
+      if (st & 1)
+        n1 = mfma32x32x16(ka[kc % 3][1], qf[kc], n1);
+      else
+        n0 = mfma32x32x16(ka[kc % 3][0], qf[kc], n0);
+      if (st > 0) stage_pack(st - 1);
+      stage_exp(st);
+      if (st + 1 < NA) stage_fma(st + 1);
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        if (i * NA / NI == st) lds_dma16(kbase + 64 * i, voff, kd + i * 4096);
+        if (i * NA / NI + NA / (2 * NI) == st) lds_dma16(vbase + 64 * i, voff, vd + i * 4096);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    stage_pack(NA - 1);
+    __builtin_amdgcn_s_setprio(0);
+    constexpr int NB = 4 * DT;          // MFMAs
+    constexpr int VB = 16 / NB > 0 ? 16 / NB : 1;  // pairs of the row max per MFMA
+    u32x4 va[3];
+    va[0] = vread(Vb, 0);
+    va[1] = vread(Vb, 1);
+    float mxn = -INFINITY;
+#pragma unroll
+    for (int jj = 0; jj < NB; ++jj) {
+      if (jj + 2 < NB) va[(jj + 2) % 3] = vread(Vb, jj + 2);
+      const int mm = jj / DT, dt = jj % DT;
+      const u32x4 b = {pb[4 * mm], pb[4 * mm + 1], pb[4 * mm + 2], pb[4 * mm + 3]};
+      acc[dt] = mfma32x32x16(va[jj % 3], b, acc[dt]);
+#pragma unroll
+      for (int u = 0; u < VB; ++u) {
+        const int e = jj * VB + u;  // pair e: elements 2e, 2e+1 of n0 (e < 8) or n1
+        const f32x16& src = e < 8 ? n0 : n1;
+        mxn = fmaxf(mxn, src[2 * (e & 7)]);
+        mxn = fmaxf(mxn, src[2 * (e & 7) + 1]);
+        asm volatile("" : "+v"(mxn));  // keeps this share of the max in its slot
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    mx_cur = mxn;
+    wait_dma();
+    __syncthreads();
+  };
+
+  const int T_main = T_full == T ? T : (T_full > 1 ? T_full - 1 : 0);
+  int t = 0;
+  for (; t + 1 < T_main; t += 2) {
+    main_iter(t, sc0, sc1, sn_0, sn_1);
+    main_iter(t + 1, sn_0, sn_1, sc0, sc1);
+  }
+  if (t < T_main) {
+    main_iter(t, sc0, sc1, sn_0, sn_1);
+    sc0 = sn_0;
+    sc1 = sn_1;
+    ++t;
+  }
+  for (; t < T; ++t) iteration(t);
+
+  const float ltot = lsum + swap_halves(lsum);
+  const int jr = 32 * wave + n;
+  if (j.row0 + jr >= j.rows) return;
+  const Row row = my_row();
+  if (j.whole && a.G == 0) {
+    if (!row.real) return;
+    const float inv = ltot != 0.f ? 1.f / ltot : 0.f;
+    const size_t at = row_index(a, j.h, row);
+    uint16_t* orow = static_cast<uint16_t*>(a.o) + at * D;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int rp = 0; rp < 2; ++rp) {
+        // the lane's channels 16rp + 4g .. +3 and 16rp + 8 + 4g .. +3 of group dt,
+        // exchanged with the lane of the other half: 8 in a row
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          w[i] = pack_bf16x2(acc[dt][8 * rp + 2 * i] * inv, acc[dt][8 * rp + 2 * i + 1] * inv);
+        const auto e0 = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+        const auto e1 = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+        stg16(orow + 32 * dt + 16 * rp + 8 * g, u32x4{e0[0], e1[0], e0[1], e1[1]});
+      }
+    if (g == 0 && a.lse != nullptr) a.lse[at] = natural_lse(m, ltot);
+    return;
+  }
+  size_t at = static_cast<size_t>(j.piece) * a.TR + jr;
+  if (j.whole)
+    at = (j.shared ? 0 : static_cast<size_t>(a.B) * a.Hkv * a.RS) + row_index(a, j.h, row);
+  float* po = (j.whole ? a.full : a.piece) + at * D;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int rg = 0; rg < 4; ++rg)
+      *reinterpret_cast<f32x4*>(po + 32 * dt + 8 * rg + 4 * g) =
+          f32x4{acc[dt][4 * rg], acc[dt][4 * rg + 1], acc[dt][4 * rg + 2], acc[dt][4 * rg + 3]};
+  if (g == 0) (j.whole ? a.full_ml : a.piece_ml)[at] = make_float2(m, ltot);
+}
+
 // ---- fp32 -------------------------------------------------------------------------------
 // 16 rows to a workgroup; its waves take 16-key pieces in turn: K through LDS buffers of
 // their own (RowTile16), V in registers, both one piece ahead, products in fp32
@@ -624,7 +989,7 @@ __device__ __forceinline__ long long run_units(const Args& a, long long total, i
   return run < a.run_min ? a.run_min : run;
 }
 
-template <int D, typename T>
+template <int D, typename T, bool MANY_SHARED, bool MANY_OWN>
 __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 prefix_attention_kernel(const Args a) {
   __shared__ __attribute__((aligned(1024))) char lds[attend_lds<D>()];
@@ -632,8 +997,8 @@ prefix_attention_kernel(const Args a) {
   __shared__ Schedule s;
   build_schedule(a, s);
   const int n = a.G + a.B;
-  const long long per_head = s.off[n], total = per_head * a.Hkv;
-  const long long run = run_units(a, total, gridDim.x);
+  const long long per_head = uniform(s.off[n]), total = per_head * a.Hkv;
+  const long long run = uniform(run_units(a, total, gridDim.x));
   if (blockIdx.x == 0 && a.sched != nullptr) {  // for the kernel that joins the rows
     for (int i = threadIdx.x; i <= n; i += kThreads) a.sched[i] = s.off[i];
     for (int i = threadIdx.x; i < a.G; i += kThreads) a.sched_sh[i] = s.sh[i];
@@ -644,7 +1009,7 @@ prefix_attention_kernel(const Args a) {
   long long u = slot * run;
   const long long stop = u + run < total ? u + run : total;
   while (u < stop) {
-    const int h = static_cast<int>(u / per_head);
+    const int h = __builtin_amdgcn_readfirstlane(static_cast<int>(u / per_head));
     const long long in = u - h * per_head;
     int lo = 0, hi = n - 1;  // the last segment that starts at or before `in` and is not empty
     while (lo < hi) {
@@ -656,7 +1021,7 @@ prefix_attention_kernel(const Args a) {
     }
     lo = __builtin_amdgcn_readfirstlane(lo);
     Job j;
-    j.h = __builtin_amdgcn_readfirstlane(h);
+    j.h = h;
     j.shared = lo < a.G;
     int tr;
     if (j.shared) {
@@ -680,7 +1045,7 @@ prefix_attention_kernel(const Args a) {
     j.pos0 = __builtin_amdgcn_readfirstlane(j.pos0);
     j.pos1 = __builtin_amdgcn_readfirstlane(j.pos1);
     const int per = ceil_div(j.pos1 - j.pos0, kTile) + kRowCost;
-    const long long x = in - s.off[lo];
+    const long long x = in - uniform(s.off[lo]);
     const int rt = __builtin_amdgcn_readfirstlane(static_cast<int>(x / per));
     const int k0 = __builtin_amdgcn_readfirstlane(
         static_cast<int>(x - static_cast<long long>(rt) * per));
@@ -691,10 +1056,19 @@ prefix_attention_kernel(const Args a) {
     j.t1 = max(k0 + take - kRowCost, 0);
     j.whole = k0 == 0 && take == per;
     j.piece = 2 * slot + (k0 > 0 ? 0 : 1);
-    if constexpr (sizeof(T) == 2)
-      attend_few<D>(a, j, lds, lds_ml);
-    else
+    if constexpr (sizeof(T) == 4) {
       attend_f32<D>(a, j, lds, lds_ml);
+    } else if constexpr (MANY_SHARED == MANY_OWN) {
+      if constexpr (MANY_OWN)
+        attend_many<D>(a, j, lds);
+      else
+        attend_few<D>(a, j, lds, lds_ml);
+    } else {
+      if (j.shared)
+        attend_many<D>(a, j, lds);
+      else
+        attend_few<D>(a, j, lds, lds_ml);
+    }
     u += take;
   }
 }
@@ -792,19 +1166,28 @@ void launch_prefix_attention(const PrefixCall& p, int dtype, int d, char* ws, hi
   a.piece_ml = reinterpret_cast<float2*>(ws + w.piece_ml);
   const size_t threads = static_cast<size_t>(p.B) * p.Hq * p.S * (d / 4);
   const dim3 cgrid = wide_grid(static_cast<long>((threads + 255) / 256));
-#define SA_PREFIX(D, T)                                                                       \
-  hipLaunchKernelGGL((prefix_attention_kernel<D, T>), dim3(kPrefixSlots), dim3(kThreads), 0, s, \
-                     a);                                                                      \
-  hipLaunchKernelGGL((prefix_combine_kernel<D, T>), cgrid, dim3(256), 0, s, a, kPrefixSlots)
-  if (dtype == 0 && d == 128) {
-    SA_PREFIX(128, uint16_t);
-  } else if (dtype == 0) {
-    SA_PREFIX(64, uint16_t);
-  } else if (d == 128) {
-    SA_PREFIX(128, float);
-  } else {
-    SA_PREFIX(64, float);
-  }
+#define SA_PREFIX(D, T, P, O)                                                                  \
+  do {                                                                                         \
+    hipLaunchKernelGGL((prefix_attention_kernel<D, T, P, O>), dim3(kPrefixSlots),              \
+                       dim3(kThreads), 0, s, a);                                               \
+    hipLaunchKernelGGL((prefix_combine_kernel<D, T>), cgrid, dim3(256), 0, s, a, kPrefixSlots); \
+  } while (0)
+#define SA_PREFIX_D(D)                        \
+  do {                                        \
+    if (dtype != 0)                           \
+      SA_PREFIX(D, float, false, false);      \
+    else if (a.TRo == kManyRows)              \
+      SA_PREFIX(D, uint16_t, true, true);     \
+    else if (a.TRp == kManyRows)              \
+      SA_PREFIX(D, uint16_t, true, false);    \
+    else                                      \
+      SA_PREFIX(D, uint16_t, false, false);   \
+  } while (0)
+  if (d == 128)
+    SA_PREFIX_D(128);
+  else
+    SA_PREFIX_D(64);
+#undef SA_PREFIX_D
 #undef SA_PREFIX
 }
 
