@@ -135,7 +135,14 @@ def _ptr(t: Optional[torch.Tensor]):
     return t.data_ptr()
 
 
+# The current stream's handle without a torch.cuda.Stream made for it (0.1 instead of
+# 2.5 us a call).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream():
+    if _raw_stream is not None:
+        return _raw_stream(torch.cuda.current_device())
     return torch.cuda.current_stream().cuda_stream
 
 

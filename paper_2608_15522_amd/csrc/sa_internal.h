@@ -314,7 +314,7 @@ struct PrefixWs {
   int shared_rows;  // rows of a row tile: shared keys,
   int own_rows;     // own keys,
   int piece_rows;   // and of a partial row tile's place
-  size_t sched, sched_sh;   // int64 [kMaxAttendSegs + 1], int [kMaxAttendSegs / 2]
+  size_t shared, parts;     // int [kMaxAttendSegs / 2], int2 [row tiles]
   size_t full, full_ml;     // float [2][B*Hq*S][d], float2 [2][B*Hq*S]; with groups only
   size_t piece, piece_ml;   // float [2 slots][piece_rows][d], float2 [2 slots][piece_rows]
   size_t total;
@@ -330,8 +330,11 @@ inline PrefixWs prefix_ws_layout(int B, int Hq, int Hkv, int S, int d, int dtype
   w.piece_rows = w.groups > 0 ? w.shared_rows : w.own_rows;
   const size_t rows = static_cast<size_t>(B) * Hq * S;
   size_t off = 0;
-  w.sched = off;    off += align_up(sizeof(long long) * (kMaxAttendSegs + 1));
-  w.sched_sh = off; off += align_up(sizeof(int) * (kMaxAttendSegs / 2));
+  w.shared = off;   off += align_up(sizeof(int) * (kMaxAttendSegs / 2));
+  w.parts = off;
+  off += align_up(sizeof(int) * 2 * Hkv * (B * ((RS + w.own_rows - 1) / w.own_rows) +
+                                           w.groups * ((RS * per + w.shared_rows - 1) /
+                                                       w.shared_rows)));
   w.full = off;     off += w.groups > 0 ? align_up(sizeof(float) * 2 * rows * d) : 0;
   w.full_ml = off;  off += w.groups > 0 ? align_up(sizeof(float) * 4 * rows) : 0;
   const size_t places = static_cast<size_t>(2) * kPrefixSlots * w.piece_rows;
@@ -339,6 +342,16 @@ inline PrefixWs prefix_ws_layout(int B, int Hq, int Hkv, int S, int d, int dtype
   w.piece_ml = off; off += align_up(sizeof(float) * 2 * places);
   w.total = off;
   return w;
+}
+// Upper bound of the units of work that a call is cut into (32 bits on the device): at most
+// 8 and two a 64-key tile for each row tile.
+inline double prefix_units(int B, int Hq, int Hkv, int S, int d, int dtype, int n_groups,
+                           long long capacity) {
+  const PrefixWs w = prefix_ws_layout(B, Hq, Hkv, S, d, dtype, n_groups);
+  const double RS = static_cast<double>(Hq / Hkv) * S;
+  const double own = B * (RS / w.own_rows + 1);
+  const double shared = w.groups > 0 ? w.groups * (B / w.groups * RS / w.shared_rows + 1) : 0;
+  return Hkv * (own + shared) * (10.0 + capacity / 32.0);
 }
 void launch_prefix_attention(const PrefixCall& p, int dtype, int d, char* ws, hipStream_t s);
 

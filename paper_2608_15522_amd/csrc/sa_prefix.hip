@@ -40,6 +40,18 @@ constexpr int kSegs = kMaxAttendSegs;
 constexpr float kRescaleSlack = 8.0f;
 constexpr float kSlackWeight = 1.f / 256.f;  // 2^-kRescaleSlack
 
+// Units of work of a row tile: `row` for what it costs whatever its keys (finding its
+// pages, the first copies' latency, its epilogue), `tile` for each 64-key tile.  A cut
+// leaves at least kSnap tiles on either side, or moves to the row tile's end.  64 samples
+// of 4 query heads a key head (8 of them) over 16384 shared tokens and up to 2000 of their
+// own at d 128 take 113 us with row costs of 4 (128 rows) and 6 (32 rows) and equal tiles,
+// 125 to 131 with tiles of the 32-row form at twice the other's, 114 the other way round.
+struct Cost {
+  int row, tile;
+};
+constexpr int kSnap = 2;
+constexpr int kRunMin = 5;  // least units of a run
+
 struct Args {
   const void* q;
   const void* kp;
@@ -55,18 +67,16 @@ struct Args {
   int n_pages, lp, max_pages, causal;
   int TRp, TRo;               // rows of a row tile: shared segments, own segments
   int TR;                     // the larger of the two: rows of a partial row tile's place
-  int run_min;                // least units of a run
+  Cost cp, co;                // units of a row tile: shared segments, own segments
   Log2Scale c;
-  long long* sched;           // [kSegs + 2] prefix sums, run
-  int* sched_sh;              // [G]
+  int* shared_out;            // [G] shared tokens that the call takes once
+  int2* parts;                // [row tiles] first slot, parts (0: none, 1: the whole tile)
+  int nrtp, nrto;             // row tiles of a segment
   float* full;                // [2][B * Hq * S][D] partial rows of whole row tiles
   float2* full_ml;            // [2][B * Hq * S]
   float* piece;               // [2 slots][TR][D] partial rows of shared row tiles
   float2* piece_ml;           // [2 slots][TR]
 };
-
-// Units that a row tile costs besides its 64-key tiles (its Q rows, its epilogue).
-constexpr int kRowCost = 1;
 
 __device__ __forceinline__ int seq_tokens(const Args& a, int b) {
   const long long cap = static_cast<long long>(a.max_pages) << a.lp;
@@ -77,32 +87,49 @@ __device__ __forceinline__ int seq_queries(const Args& a, int b) {
   return a.q_len != nullptr ? min(max(a.q_len[b], 0), a.S) : a.S;
 }
 
-__device__ __forceinline__ long long uniform(long long x) {
-  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x));
-  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x >> 32));
-  return static_cast<long long>((static_cast<uint64_t>(hi) << 32) | lo);
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// x / y for 0 <= x < 2^31, y > 0 and a quotient below 2^20, inv = 1.f / y: the product is
+// off by less than one.
+__device__ __forceinline__ int div_small(int x, int y, float inv) {
+  int q = static_cast<int>(static_cast<float>(x) * inv);
+  q -= q * y > x;
+  q += (q + 1) * y <= x;
+  return q;
 }
 
-// Prefix sums of the segments' units of one head, and the shared tokens of each group:
-// whole pages, at most what every sequence with a key has and (causal) what its first
-// query sees.
+// Prefix sums of the segments' units of one head, the sequences' lengths, and the shared
+// tokens of each group: whole pages, at most what every sequence with a key has and
+// (causal) what its first query sees.
 struct Schedule {
-  long long off[kSegs + 1];
+  int off[kSegs + 1];
+  int wave_tot[kWaves];
+  int len[kSegs];
   int sh[kSegs / 2];
-  long long wave_tot[kWaves];
+  int most;  // units of the longest row tile
 };
+
+__device__ __forceinline__ Cost cost_of(const Args& a, bool shared) {
+  return Cost{shared ? a.cp.row : a.co.row, shared ? a.cp.tile : a.co.tile};
+}
+__device__ __forceinline__ int row_units(const Cost& c, int keys) {
+  return c.row + c.tile * ceil_div(keys, kTile);
+}
 
 __device__ void build_schedule(const Args& a, Schedule& s) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  for (int g = tid; g < a.G; g += kThreads) s.sh[g] = 0x7fffffff;
+  if (tid == 0) s.most = 0;
+  __syncthreads();
+  for (int b = tid; b < a.B; b += kThreads) {
+    const int len = seq_tokens(a, b);
+    s.len[b] = len;
+    if (a.G == 0) atomicMax(&s.most, row_units(a.co, len));
+    if (a.G > 0 && len > 0)
+      atomicMin(&s.sh[b / a.N], a.causal ? max(min(len - seq_queries(a, b) + 1, len), 0) : len);
+  }
+  __syncthreads();
   if (a.G > 0) {
-    for (int g = tid; g < a.G; g += kThreads) s.sh[g] = 0x7fffffff;
-    __syncthreads();
-    for (int b = tid; b < a.B; b += kThreads) {
-      const int len = seq_tokens(a, b);
-      if (len > 0)
-        atomicMin(&s.sh[b / a.N], a.causal ? max(min(len - seq_queries(a, b) + 1, len), 0) : len);
-    }
-    __syncthreads();
     for (int g = tid; g < a.G; g += kThreads) {
       // no sequence of the group has a key: nothing to share
       const int v = s.sh[g] == 0x7fffffff ? 0 : min(s.sh[g], max(a.shared_len[g], 0));
@@ -112,26 +139,22 @@ __device__ void build_schedule(const Args& a, Schedule& s) {
   }
   const int n = a.G + a.B, each = ceil_div(n, kThreads);
   const int i0 = min(tid * each, n), i1 = min(i0 + each, n);
-  auto units = [&](int i) -> long long {
-    if (i < a.G) {
-      const int nk = ceil_div(s.sh[i], kTile);
-      return nk == 0 ? 0 : static_cast<long long>(ceil_div(a.N * a.RS, a.TRp)) * (nk + kRowCost);
-    }
-    const int b = i - a.G, len = seq_tokens(a, b);
-    const int own = a.G > 0 ? max(len - s.sh[b / a.N], 0) : len;
-    return static_cast<long long>(ceil_div(a.RS, a.TRo)) * (ceil_div(own, kTile) + kRowCost);
+  auto units = [&](int i) {
+    if (i < a.G) return s.sh[i] == 0 ? 0 : a.nrtp * row_units(a.cp, s.sh[i]);
+    const int b = i - a.G;
+    return a.nrto * row_units(a.co, a.G > 0 ? max(s.len[b] - s.sh[b / a.N], 0) : s.len[b]);
   };
-  long long sum = 0;
+  int sum = 0;
   for (int i = i0; i < i1; ++i) sum += units(i);
-  long long incl = sum;
+  int incl = sum;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const long long u = __shfl_up(incl, o, 64);
+    const int u = __shfl_up(incl, o, 64);
     if (lane >= o) incl += u;
   }
   if (lane == 63) s.wave_tot[wave] = incl;
   __syncthreads();
-  long long at = incl - sum;
+  int at = incl - sum;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w)
     if (w < wave) at += s.wave_tot[w];
@@ -157,19 +180,20 @@ struct Job {
   int piece;        // place of the partial rows if not
 };
 
-// Row rho of a segment: sequence, row within (sequence, key head), whether it exists.
+// Row rho of a segment: sequence, row within (sequence, key head), whether the segment has
+// it, and whether it holds a query.
 struct Row {
   int b, in;
-  bool real;
+  bool inside, real;
 };
 __device__ __forceinline__ Row row_of(const Args& a, const Job& j, int rho) {
   Row r;
-  const bool inside = rho < j.rows;
-  rho = inside ? rho : j.rows - 1;
+  r.inside = rho < j.rows;
+  rho = r.inside ? rho : j.rows - 1;
   const int k = j.shared ? rho / a.RS : 0;
   r.b = j.b0 + k;
   r.in = rho - k * a.RS;
-  r.real = inside && r.in % a.S < seq_queries(a, r.b);
+  r.real = r.inside && r.in % a.S < seq_queries(a, r.b);
   return r;
 }
 __device__ __forceinline__ size_t row_index(const Args& a, int h, const Row& r) {
@@ -330,14 +354,18 @@ __device__ void attend_few(const Args& a, const Job& j, char* lds_all, float2* l
 
   const Row row = row_of(a, j, j.row0 + n);
   const uint16_t* q = static_cast<const uint16_t*>(a.q);
+  const int run0 = j.pos0 + kTile * j.t0, run1 = min(j.pos1, j.pos0 + kTile * j.t1);
+  const int first = run0 + kPiece * wave;
+  // loads that do not wait for one another go out together: table entries, Q
+  PageCursor cur;
+  cur.start(a, j.pages, min(first, max(run1 - 1, 0)));
   u32x4 qf[KC];
 #pragma unroll
   for (int kc = 0; kc < KC; ++kc)
-    qf[kc] = row.real ? ldg16(q + row_index(a, j.h, row) * D + 16 * kc + 8 * g)
-                      : u32x4{0u, 0u, 0u, 0u};
-  const int end = row_end(a, j, row);
-  const int run0 = j.pos0 + kTile * j.t0, run1 = min(j.pos1, j.pos0 + kTile * j.t1);
+    qf[kc] = row.inside ? ldg16(q + row_index(a, j.h, row) * D + 16 * kc + 8 * g)
+                        : u32x4{0u, 0u, 0u, 0u};
   const bool bad = bad_pages(a, j.pages, run0, run1);
+  const int end = row_end(a, j, row);
 
   // DMA: 1 KB = 16 rows of one 32-channel plane; lane l's source is the 16-byte slot that
   // the swizzle keeps at slot l % 4 of row l / 4.
@@ -352,9 +380,6 @@ __device__ void attend_few(const Args& a, const Job& j, char* lds_all, float2* l
   const int v_off1 = (8 + tr_key) * 64 + 16 * ((tr_byte >> 4) ^ plane_swz(8 + tr_key)) +
                      (tr_byte & 15);
 
-  const int first = run0 + kPiece * wave;
-  PageCursor cur;
-  cur.start(a, j.pages, min(first, max(run1 - 1, 0)));
   size_t off[2];  // byte offsets of the piece's two 16-row groups, the same in K and V
   auto look = [&](int pos) {
 #pragma unroll
@@ -509,7 +534,7 @@ __device__ void attend_many(const Args& a, const Job& j, char* lds) {
     const uint16_t* q = static_cast<const uint16_t*>(a.q) + row_index(a, j.h, row) * D + 8 * g;
 #pragma unroll
     for (int kc = 0; kc < KC; ++kc)
-      qf[kc] = row.real ? ldg16(q + 16 * kc) : u32x4{0u, 0u, 0u, 0u};
+      qf[kc] = row.inside ? ldg16(q + 16 * kc) : u32x4{0u, 0u, 0u, 0u};
   }
   const int run0 = j.pos0 + kTile * j.t0, run1 = min(j.pos1, j.pos0 + kTile * j.t1);
   int most = run1, least = run1;       // the furthest and the nearest end of the tile's rows
@@ -860,17 +885,17 @@ __device__ void attend_f32(const Args& a, const Job& j, char* lds_all, float2* l
   char* lds = lds_all + wave * 2 * KTile::kBytes;
   const Row row = row_of(a, j, j.row0 + n);
   const float* q = static_cast<const float*>(a.q);
-  f32x4 qf[KI];
-#pragma unroll
-  for (int i = 0; i < KI; ++i)
-    qf[i] = row.real ? ldg_f32x4(q + row_index(a, j.h, row) * D + 16 * i + 4 * gk)
-                     : f32x4{0.f, 0.f, 0.f, 0.f};
-  const int end = row_end(a, j, row);
   const int run0 = j.pos0 + kTile * j.t0, run1 = min(j.pos1, j.pos0 + kTile * j.t1);
-  const bool bad = bad_pages(a, j.pages, run0, run1);
   const int first = run0 + kF32Keys * wave;
   PageCursor cur;
   cur.start(a, j.pages, min(first, max(run1 - 1, 0)));
+  f32x4 qf[KI];
+#pragma unroll
+  for (int i = 0; i < KI; ++i)
+    qf[i] = row.inside ? ldg_f32x4(q + row_index(a, j.h, row) * D + 16 * i + 4 * gk)
+                       : f32x4{0.f, 0.f, 0.f, 0.f};
+  const bool bad = bad_pages(a, j.pages, run0, run1);
+  const int end = row_end(a, j, row);
   KTile kt;
   kt.init(lds, lane);
   struct Piece {
@@ -982,80 +1007,185 @@ constexpr int attend_lds() {
 }
 
 // ---- the runs ---------------------------------------------------------------------------
-// The units of a run, and the run of a unit.  Runs of one slot each; equal but for the
-// last ones of a small call.
-__device__ __forceinline__ long long run_units(const Args& a, long long total, int slots) {
-  const long long run = (total + slots - 1) / slots;
-  return run < a.run_min ? a.run_min : run;
+// Run c is units [c * run, (c + 1) * run), its ends moved to a row tile's end where they
+// would leave less than kSnap tiles on either side.
+__device__ __forceinline__ int run_units(int total, int slots) {
+  const int run = ceil_div(total, slots);
+  return run < kRunMin ? kRunMin : run;
+}
+
+// Where unit u lies: its head, segment, row tile, the units of the row tile before it, and
+// those of the row tile.
+struct Place {
+  int h, seg, rt, k, per;
+};
+__device__ __forceinline__ Place place_of(const Args& a, const Schedule& s, int per_head,
+                                          float inv_head, int u) {
+  const int lane = threadIdx.x & 63, n = a.G + a.B;
+  Place p;
+  p.h = uniform(div_small(u, per_head, inv_head));
+  const int in = u - p.h * per_head;
+  int before = 0;  // segments that start at or before `in`: the last of them is not empty
+  for (int i = 0; i < n; i += 64) before += __popcll(__ballot(i + lane < n && s.off[i + lane] <= in));
+  p.seg = uniform(before) - 1;
+  const int b = p.seg - a.G;
+  const int keys = p.seg < a.G ? s.sh[p.seg]
+                               : a.G > 0 ? max(s.len[b] - s.sh[b / a.N], 0) : s.len[b];
+  p.per = uniform(row_units(cost_of(a, p.seg < a.G), keys));
+  const int x = in - s.off[p.seg];
+  p.rt = uniform(x / p.per);
+  p.k = uniform(x) - p.rt * p.per;
+  return p;
+}
+// Whether a row tile may be cut at its unit k.
+__device__ __forceinline__ bool cuts(const Cost& c, int per, int k) {
+  return k >= c.row + kSnap * c.tile && k <= per - kSnap * c.tile;
+}
+
+// How the row tiles reach the workgroups: kRuns as above; kWhole one row tile a workgroup,
+// every one written out at once.  In kRuns, if no sequence's rows take much longer than the
+// mean and there are as many row tiles as slots, each slot first takes whole row tiles, in
+// rounds of all slots of an XCD, and only the rest is cut (kRounds): the workgroups of a
+// round go through a head's keys side by side, so that these come from the XCD's L2.  16
+// heads of 4 x 1024 queries over 16000 keys (a whole row tile a slot) run at 920 TFLOP/s, 20
+// heads cut into equal runs at 740.
+enum Split { kRuns, kWhole };
+
+// Row tile t of a call without shared segments: head by head, the last rows first (under a
+// causal mask they see the most keys), sequence by sequence.
+struct Tile {
+  int h, b, rt;
+};
+__device__ __forceinline__ Tile tile_of(const Args& a, int t) {
+  const int per = a.B * a.nrto;
+  Tile x;
+  x.h = uniform(t / per);
+  const int in = t - x.h * per, q = uniform(in / a.B);
+  x.rt = a.nrto - 1 - q;
+  x.b = in - q * a.B;
+  return x;
 }
 
 template <int D, typename T, bool MANY_SHARED, bool MANY_OWN>
 __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
-prefix_attention_kernel(const Args a) {
+prefix_attention_kernel(const Args a, Split split) {
   __shared__ __attribute__((aligned(1024))) char lds[attend_lds<D>()];
-  __shared__ float2 lds_ml[kWaves * 32];
+  __shared__ float2 lds_ml[kWaves * kJoinRows];
   __shared__ Schedule s;
-  build_schedule(a, s);
-  const int n = a.G + a.B;
-  const long long per_head = uniform(s.off[n]), total = per_head * a.Hkv;
-  const long long run = uniform(run_units(a, total, gridDim.x));
-  if (blockIdx.x == 0 && a.sched != nullptr) {  // for the kernel that joins the rows
-    for (int i = threadIdx.x; i <= n; i += kThreads) a.sched[i] = s.off[i];
-    for (int i = threadIdx.x; i < a.G; i += kThreads) a.sched_sh[i] = s.sh[i];
-  }
+  const int lane = threadIdx.x & 63;
+  const int xcd = blockIdx.x & 7, in_xcd = blockIdx.x >> 3, slots_xcd = gridDim.x >> 3;
   // consecutive runs on one XCD, so that row tiles of a head share their keys in its L2
-  const int per_xcd = gridDim.x >> 3;
-  const int slot = (gridDim.x & 7) != 0 ? blockIdx.x : (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-  long long u = slot * run;
-  const long long stop = u + run < total ? u + run : total;
-  while (u < stop) {
-    const int h = __builtin_amdgcn_readfirstlane(static_cast<int>(u / per_head));
-    const long long in = u - h * per_head;
-    int lo = 0, hi = n - 1;  // the last segment that starts at or before `in` and is not empty
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (s.off[mid] <= in)
-        lo = mid;
-      else
-        hi = mid - 1;
+  const int slot = xcd * slots_xcd + in_xcd;
+  const int nt = a.Hkv * a.B * a.nrto;
+  const bool whole = split == kWhole;
+  bool rounds = false;
+  int per_head = 1, total = 0;
+  float inv_head = 1.f;
+  if (!whole) {
+    build_schedule(a, s);
+    per_head = uniform(s.off[a.G + a.B]);
+    total = per_head * a.Hkv;
+    inv_head = 1.f / static_cast<float>(per_head);
+    if (blockIdx.x == 0)
+      for (int i = threadIdx.x; i < a.G; i += kThreads) a.shared_out[i] = s.sh[i];
+    rounds = a.G == 0 && nt >= kPrefixSlots &&
+             uniform(s.most) <= 1.25f * static_cast<float>(total) / static_cast<float>(nt);
+  }
+  // Rounds: row tiles [t, end) of the XCD, slots_xcd at a time.  What remains then, less than
+  // one row tile a slot, is kept a row tile a lane (slots_xcd is 64): units `per_l`, `upto`
+  // with those of the lanes before.
+  int t = slot, end = nt, rest = 0, per_l = 0, upto = 0;
+  if (rounds) {
+    t = static_cast<int>(static_cast<long long>(nt) * xcd / kXcds);
+    end = static_cast<int>(static_cast<long long>(nt) * (xcd + 1) / kXcds);
+    rest = t + (end - t) / slots_xcd * slots_xcd;
+    if (rest + lane < end)
+      per_l = row_units(a.co, s.len[(rest + lane) % (a.B * a.nrto) % a.B]);
+    upto = per_l;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(upto, o, 64);
+      if (lane >= o) upto += v;
     }
-    lo = __builtin_amdgcn_readfirstlane(lo);
-    Job j;
-    j.h = h;
-    j.shared = lo < a.G;
-    int tr;
-    if (j.shared) {
-      j.b0 = lo * a.N;
-      j.rows = a.N * a.RS;
-      j.pos0 = 0;
-      j.pos1 = s.sh[lo];
-      tr = a.TRp;
-      int rep = j.b0;  // the group's first sequence with a key
-      while (rep + 1 < j.b0 + a.N && seq_tokens(a, rep) == 0) ++rep;
-      j.pages = a.table + static_cast<size_t>(rep) * a.max_pages;
+    total = uniform(__shfl(upto, 63, 64));
+    t += in_xcd;
+  }
+  // The run: units [u, stop) of the call or, after the rounds, of the XCD's rest.
+  const int my = rounds ? in_xcd : slot;
+  const int run = whole ? 1 : run_units(total, rounds ? slots_xcd : kPrefixSlots);
+  auto place = [&](int x) {
+    if (!rounds) return place_of(a, s, per_head, inv_head, x);
+    Place p;
+    const int i = uniform(__popcll(__ballot(upto <= x)));
+    p.per = __builtin_amdgcn_readlane(per_l, i);
+    p.k = x - (__builtin_amdgcn_readlane(upto, i) - p.per);
+    const Tile y = tile_of(a, rest + i);
+    p.h = y.h;
+    p.seg = y.b;
+    p.rt = y.rt;
+    return p;
+  };
+  // an end inside a row tile where it is not cut moves to the tile's beginning or end
+  auto settle = [&](int x) {
+    const Place p = place(x);
+    const Cost c = cost_of(a, p.seg < a.G);
+    if (cuts(c, p.per, p.k)) return x;
+    return p.k < c.row + kSnap * c.tile ? x - p.k : x - p.k + p.per;
+  };
+  int u = 0, stop = 0;
+  if (!whole && my < ceil_div(total, run)) {
+    u = my > 0 ? settle(my * run) : 0;
+    stop = total - my * run > run ? settle(my * run + run) : total;
+  }
+  for (;;) {
+    Place p;
+    int take, last = 0;  // slots behind this one that hold parts of a row tile begun here
+    if ((whole && t < end) || (rounds && t < rest)) {
+      const Tile x = tile_of(a, t);
+      p = Place{x.h, a.G + x.b, x.rt, 0, row_units(a.co, whole ? 0 : s.len[x.b])};
+      take = p.per;
+      t = whole ? end : t + slots_xcd;
+    } else if (u < stop) {
+      p = place(u);
+      take = min(stop - u, p.per - p.k);
+      // those whose runs begin inside the row tile
+      if (take < p.per)
+        last = (u - p.k + p.per - kSnap * cost_of(a, p.seg < a.G).tile) / run - my;
+      u += take;
     } else {
-      j.b0 = lo - a.G;
-      j.rows = a.RS;
-      const int len = seq_tokens(a, j.b0);
-      j.pos0 = a.G > 0 ? min(s.sh[j.b0 / a.N], len) : 0;
-      j.pos1 = len;
-      tr = a.TRo;
-      j.pages = a.table + static_cast<size_t>(j.b0) * a.max_pages;
+      break;
     }
-    j.pos0 = __builtin_amdgcn_readfirstlane(j.pos0);
-    j.pos1 = __builtin_amdgcn_readfirstlane(j.pos1);
-    const int per = ceil_div(j.pos1 - j.pos0, kTile) + kRowCost;
-    const long long x = in - uniform(s.off[lo]);
-    const int rt = __builtin_amdgcn_readfirstlane(static_cast<int>(x / per));
-    const int k0 = __builtin_amdgcn_readfirstlane(
-        static_cast<int>(x - static_cast<long long>(rt) * per));
-    const int take = __builtin_amdgcn_readfirstlane(
-        static_cast<int>(stop - u < per - k0 ? stop - u : per - k0));
-    j.row0 = rt * tr;
-    j.t0 = max(k0 - kRowCost, 0);
-    j.t1 = max(k0 + take - kRowCost, 0);
-    j.whole = k0 == 0 && take == per;
-    j.piece = 2 * slot + (k0 > 0 ? 0 : 1);
+    const Cost c = cost_of(a, p.seg < a.G);
+    Job j;
+    int tile;  // the row tile's number in `parts`
+    j.h = p.h;
+    j.shared = p.seg < a.G;
+    if (j.shared) {
+      j.b0 = p.seg * a.N;
+      j.rows = a.N * a.RS;
+      j.row0 = p.rt * a.TRp;
+      j.pos0 = 0;
+      j.pos1 = uniform(s.sh[p.seg]);
+      int rep = j.b0;  // the group's first sequence with a key
+      while (rep + 1 < j.b0 + a.N && s.len[rep] == 0) ++rep;
+      j.pages = a.table + static_cast<size_t>(uniform(rep)) * a.max_pages;
+      tile = (p.seg * a.Hkv + p.h) * a.nrtp + p.rt;
+    } else {
+      j.b0 = p.seg - a.G;
+      const int len = whole ? seq_tokens(a, j.b0) : s.len[j.b0];
+      j.rows = a.RS;
+      j.row0 = p.rt * a.TRo;
+      j.pos0 = uniform(a.G > 0 ? min(s.sh[j.b0 / a.N], len) : 0);
+      j.pos1 = uniform(len);
+      j.pages = a.table + static_cast<size_t>(j.b0) * a.max_pages;
+      tile = a.G * a.Hkv * a.nrtp + (j.b0 * a.Hkv + p.h) * a.nrto + p.rt;
+    }
+    j.t0 = uniform(max(p.k - c.row, 0) / c.tile);
+    j.t1 = uniform(whole ? ceil_div(j.pos1, kTile) : max(p.k + take - c.row, 0) / c.tile);
+    j.whole = take == p.per;
+    j.piece = 2 * slot + (p.k > 0 ? 0 : 1);
+    if (!whole && p.k == 0 && threadIdx.x == 0)
+      a.parts[tile] = make_int2(slot, j.pos1 == j.pos0 ? 0 : last + 1);
     if constexpr (sizeof(T) == 4) {
       attend_f32<D>(a, j, lds, lds_ml);
     } else if constexpr (MANY_SHARED == MANY_OWN) {
@@ -1069,63 +1199,111 @@ prefix_attention_kernel(const Args a) {
       else
         attend_few<D>(a, j, lds, lds_ml);
     }
-    u += take;
   }
 }
 
-// Joins the partial rows of every row: those of the shared keys, then those of its own, in
-// key order.  4 channels of a row a thread.
-template <int D, typename T>
-__global__ void __launch_bounds__(256)
-prefix_combine_kernel(const Args a, int slots) {
-  constexpr int TPR = D / 4;
-  const size_t gid =
-      (static_cast<size_t>(blockIdx.z) * gridDim.x + blockIdx.x) * 256 + threadIdx.x;
-  const size_t row = gid / TPR, rows = static_cast<size_t>(a.B) * a.Hkv * a.RS;
-  if (row >= rows) return;
-  const int c4 = static_cast<int>(gid % TPR);
-  const size_t bh = row / a.RS;
-  const int in = static_cast<int>(row - bh * a.RS);
-  const int b = static_cast<int>(bh / a.Hkv), h = static_cast<int>(bh - static_cast<size_t>(b) * a.Hkv);
-  if (in % a.S >= seq_queries(a, b)) return;
-  const int n = a.G + a.B, len = seq_tokens(a, b);
-  const long long per_head = a.sched[n], total = per_head * a.Hkv;
-  const long long run = run_units(a, total, slots);
-  float M = -FLT_MAX, den = 0.f;
-  f32x4 num = {0.f, 0.f, 0.f, 0.f};
-  auto add = [&](const float* o, float2 ml) {
-    if (ml.y == 0.f) return;
-    const float m = fmaxf(M, ml.x), fa = fast_exp2(M - m), fb = fast_exp2(ml.x - m);
-    const f32x4 x = ldg_f32x4(o + 4 * c4);
-    M = m;
-    den = fmaf(fb, ml.y, fa * den);
+// Joins the partial rows of every row that has some: those of the shared keys, then those
+// of its own, in key order.  Workgroup (x, h, b) takes `chunk` rows of a (sequence, key
+// head); PG groups of D / 4 threads share a row, each taking every PG-th part, four parts'
+// loads at a time, and their sums are joined in group order.  Latency-bound: two loads in
+// turn.
+constexpr int kCombineThreads = 256;
+template <int D, typename T, int PG>
+__global__ void __launch_bounds__(kCombineThreads)
+prefix_combine_kernel(const Args a, int chunk) {
+  constexpr int TPR = D / 4, RA = kCombineThreads / (TPR * PG);  // rows at once
+  __shared__ f32x4 sum_num[PG > 1 ? kCombineThreads : 1];
+  __shared__ float2 sum_ml[PG > 1 ? RA * PG : 1];
+  const int tid = threadIdx.x;
+  const int c4 = tid % TPR, pg = tid / TPR % PG, ra = tid / (TPR * PG);
+  const int b = blockIdx.z, h = blockIdx.y, pair = b * a.Hkv + h;
+  const int first_row = blockIdx.x * chunk, last_row = min(first_row + chunk, a.RS);
+  const int2* own = a.parts + a.G * a.Hkv * a.nrtp + pair * a.nrto;
+  // one row tile, and written already unless it is cut
+  if (a.G == 0 && chunk <= a.TRo && own[first_row / a.TRo].y <= 1) return;
+  const int nq = seq_queries(a, b), len = a.seq_len[b];
+  const int g = a.G > 0 ? b / a.N : 0;
+  const bool shared = a.G > 0 && len > 0 && a.shared_out[g] > 0;
+  const size_t rows = static_cast<size_t>(a.B) * a.Hkv * a.RS;
+  for (int r0 = first_row; r0 < last_row; r0 += RA) {
+    const int in = min(r0 + ra, a.RS - 1);
+    const bool real = r0 + ra < last_row && in % a.S < nq;
+    const size_t row = static_cast<size_t>(pair) * a.RS + in;
+    const int2 po = own[in / a.TRo];
+    const int rho = (b - g * a.N) * a.RS + in;  // among the group's rows
+    const int2 ps = shared ? a.parts[(g * a.Hkv + h) * a.nrtp + rho / a.TRp] : make_int2(0, 0);
+    const int np = ps.y + po.y;
+    const bool mine = real && (a.G > 0 || po.y > 1);  // else it is written already
+    float M = -FLT_MAX, den = 0.f;
+    f32x4 num = {0.f, 0.f, 0.f, 0.f};
+    if (mine) {
+      auto part = [&](int i, f32x4* x) {
+        const bool of_shared = i < ps.y;
+        const int2 p = of_shared ? ps : po;
+        const int k = of_shared ? i : i - ps.y;  // part k of the row tile
+        const bool whole = p.y == 1;
+        const size_t place = static_cast<size_t>(2) * (p.x + k) + (k == 0 ? 1 : 0);
+        const size_t at = whole ? (of_shared ? 0 : rows) + row
+                                : place * a.TR + (of_shared ? rho % a.TRp : in % a.TRo);
+        *x = ldg_f32x4((whole ? a.full : a.piece) + at * D + 4 * c4);
+        return (whole ? a.full_ml : a.piece_ml)[at];
+      };
+      for (int i0 = pg; i0 < np; i0 += 4 * PG) {
+        f32x4 x[4];
+        float2 ml[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) num[e] = fmaf(fb, x[e], fa * num[e]);
-  };
-  auto segment = [&](int seg, int keys, int rho, int tr, size_t full_at) {
-    const int per = ceil_div(keys, kTile) + kRowCost;
-    const long long u0 = h * per_head + a.sched[seg] + static_cast<long long>(rho / tr) * per;
-    const int first = static_cast<int>(u0 / run), last = static_cast<int>((u0 + per - 1) / run);
-    if (first == last) {
-      if (a.G > 0) add(a.full + full_at * D, a.full_ml[full_at]);
-      return a.G > 0;
+        for (int e = 0; e < 4; ++e) ml[e] = part(min(i0 + e * PG, np - 1), &x[e]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (i0 + e * PG >= np || ml[e].y == 0.f) continue;
+          const float m = fmaxf(M, ml[e].x), fa = fast_exp2(M - m), fb = fast_exp2(ml[e].x - m);
+          M = m;
+          den = fmaf(fb, ml[e].y, fa * den);
+#pragma unroll
+          for (int w = 0; w < 4; ++w) num[w] = fmaf(fb, x[e][w], fa * num[w]);
+        }
+      }
     }
-    for (int s = first; s <= last; ++s) {
-      const size_t at = static_cast<size_t>(2 * s + (s == first ? 1 : 0)) * a.TR + rho % tr;
-      // a run that starts with the row tile's first unit holds it from its beginning
-      add(a.piece + at * D, a.piece_ml[at]);
+    if constexpr (PG > 1) {
+      sum_num[tid] = num;
+      if (c4 == 0) sum_ml[ra * PG + pg] = make_float2(M, den);
+      __syncthreads();
+      if (pg == 0) {
+#pragma unroll
+        for (int w = 1; w < PG; ++w) {
+          const float2 ml = sum_ml[ra * PG + w];
+          if (ml.y == 0.f) continue;
+          const f32x4 x = sum_num[tid + w * TPR];
+          const float m = fmaxf(M, ml.x), fa = fast_exp2(M - m), fb = fast_exp2(ml.x - m);
+          M = m;
+          den = fmaf(fb, ml.y, fa * den);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) num[e] = fmaf(fb, x[e], fa * num[e]);
+        }
+      }
+      __syncthreads();
     }
-    return true;
-  };
-  if (len > 0) {
-    const int g = a.G > 0 ? b / a.N : 0;
-    const int sh = a.G > 0 ? a.sched_sh[g] : 0;
-    if (sh > 0) segment(g, sh, (b - g * a.N) * a.RS + in, a.TRp, row);
-    if (!segment(a.G + b, len - sh, in, a.TRo, rows + row)) return;  // written already
-  } else if (a.G == 0) {
-    return;
+    if (mine && pg == 0) store_row<D, T>(a, row, c4, num, M, den);
   }
-  store_row<D, T>(a, row, c4, num, M, den);
+}
+
+// Whether every row tile goes to a workgroup of its own, which saves finding the runs and
+// the joining kernel (some 6 us), by the keys that a table row has room for.  One workgroup
+// takes 4 to 6 us a thousand keys, so up to 1024 keys it is as fast as runs however few the
+// row tiles: 24 heads of 2 sequences (48 row tiles) at d 128 take 16.1 against 21.4 us with
+// room for 1000 keys, 27.5 against 23.6 with room for 2000; with at least as many row tiles
+// as slots up to 2048 (720 row tiles: 86 against 89 us; 162 against 150 for 4000); and with
+// eight times as many at any length, since these even out by themselves (4800 row tiles,
+// 1000 keys: 230 against 255 us).  Under a causal mask the row tiles of a sequence whose
+// queries are a quarter of its tokens or more see unequally many keys, which runs do not
+// know: as many row tiles as slots suffice (528 of up to 1700 keys: 51 against 62 us).  Where sequences share tokens, reading these once for all is given up only
+// for so few keys that the L2 makes up for it.
+bool whole_tiles(const Args& a, const PrefixCall& p) {
+  const long long tiles = static_cast<long long>(a.Hkv) * a.B * a.nrto;
+  const long long keys = static_cast<long long>(p.max_pages) * p.page;
+  if (a.G > 0) return keys <= 1024 && tiles * keys <= 1 << 17;
+  return keys <= 1024 || (tiles >= kPrefixSlots && (keys <= 2048 || (p.causal && keys <= 4ll * p.S))) ||
+         tiles >= 8 * kPrefixSlots;
 }
 
 }  // namespace
@@ -1156,21 +1334,40 @@ void launch_prefix_attention(const PrefixCall& p, int dtype, int d, char* ws, hi
   a.TRp = w.shared_rows;
   a.TRo = w.own_rows;
   a.TR = w.piece_rows;
-  a.run_min = 4;
+  const auto cost = [&](int rows) { return rows == kManyRows ? Cost{4, 1} : Cost{6, 1}; };
+  a.cp = cost(a.TRp);
+  a.co = cost(a.TRo);
   a.c = log2_scale(p.scale);
-  a.sched = reinterpret_cast<long long*>(ws + w.sched);
-  a.sched_sh = reinterpret_cast<int*>(ws + w.sched_sh);
+  a.shared_out = reinterpret_cast<int*>(ws + w.shared);
+  a.parts = reinterpret_cast<int2*>(ws + w.parts);
+  a.nrtp = w.groups > 0 ? ceil_div(a.N * a.RS, a.TRp) : 0;
+  a.nrto = ceil_div(a.RS, a.TRo);
   a.full = reinterpret_cast<float*>(ws + w.full);
   a.full_ml = reinterpret_cast<float2*>(ws + w.full_ml);
   a.piece = reinterpret_cast<float*>(ws + w.piece);
   a.piece_ml = reinterpret_cast<float2*>(ws + w.piece_ml);
-  const size_t threads = static_cast<size_t>(p.B) * p.Hq * p.S * (d / 4);
-  const dim3 cgrid = wide_grid(static_cast<long>((threads + 255) / 256));
+  // threads that share a row in the joining kernel: eight times as many where a row tile may
+  // be cut into 16 parts and more
+  const long tiles = a.G > 0 ? static_cast<long>(a.G) * a.Hkv * a.nrtp
+                             : static_cast<long>(a.B) * a.Hkv * a.nrto;
+  const bool share = kPrefixSlots / tiles >= 16;
+  const int at_once = kCombineThreads / (d / 4) / (share ? 8 : 1);
+  const int chunk = a.G == 0 && !share ? (a.TRo < 32 ? a.TRo : 32) : at_once;
+  const dim3 cgrid(ceil_div(a.RS, chunk), a.Hkv, a.B);
+  const Split split = whole_tiles(a, p) ? kWhole : kRuns;
+  if (split == kWhole) a.G = 0;
+  const int wgs = split == kWhole ? kXcds * ceil_div(a.Hkv * a.B * a.nrto, kXcds) : kPrefixSlots;
 #define SA_PREFIX(D, T, P, O)                                                                  \
   do {                                                                                         \
-    hipLaunchKernelGGL((prefix_attention_kernel<D, T, P, O>), dim3(kPrefixSlots),              \
-                       dim3(kThreads), 0, s, a);                                               \
-    hipLaunchKernelGGL((prefix_combine_kernel<D, T>), cgrid, dim3(256), 0, s, a, kPrefixSlots); \
+    hipLaunchKernelGGL((prefix_attention_kernel<D, T, P, O>), dim3(wgs), dim3(kThreads), 0, s, a, \
+                       split);                                                                 \
+    if (split == kWhole) break;                                                                \
+    if (share)                                                                                 \
+      hipLaunchKernelGGL((prefix_combine_kernel<D, T, 8>), cgrid, dim3(kCombineThreads), 0, s, a, \
+                         chunk);                                                               \
+    else                                                                                       \
+      hipLaunchKernelGGL((prefix_combine_kernel<D, T, 1>), cgrid, dim3(kCombineThreads), 0, s, a, \
+                         chunk);                                                               \
   } while (0)
 #define SA_PREFIX_D(D)                        \
   do {                                        \
