@@ -151,7 +151,7 @@ def _expect(t, name, shape, dtype):
     the call implies would be read or written out of bounds, so refuse it."""
     if t is None:
         return
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != tuple(shape):
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
     if t.dtype != dtype:
         raise TypeError(f"{name}: dtype {t.dtype}, expected {dtype}")
@@ -504,13 +504,13 @@ def sa_cache_indicator(y_v, y_v_hat, *, prot_flag=None, y_a=None, y_a_hat=None,
 def _here(*tensors):
     """The calls go to the current device's current stream: a tensor of another
     device is refused."""
-    dev = tensors[0].device
+    first = tensors[0]
+    index = first.get_device()  # -1 on the CPU
     for t in tensors:
-        if t is not None and t.device != dev:
-            raise ValueError(f"tensors on {dev} and {t.device}")
-    if dev.type == "cuda" and dev.index != torch.cuda.current_device():
-        raise ValueError(f"tensors on {dev}, which is not the current device")
-    return dev
+        if t is not None and t.get_device() != index:
+            raise ValueError(f"tensors on {first.device} and {t.device}")
+    if index >= 0 and index != torch.cuda.current_device():
+        raise ValueError(f"tensors on {first.device}, which is not the current device")
 
 
 def _table(page_table, seq_len, page_ref=None):
@@ -531,9 +531,9 @@ def sa_pages_reserve(page_table, seq_len, page_ref, n_new, page, *, missing=None
     B, max_pages = _table(page_table, seq_len, page_ref)
     _expect(n_new, "n_new", (B,), torch.int32)
     _expect(missing, "missing", (1,), torch.int32)
-    dev = _here(page_table, seq_len, page_ref, n_new, missing)
+    _here(page_table, seq_len, page_ref, n_new, missing)
     if missing is None:
-        missing = torch.empty(1, dtype=torch.int32, device=dev)
+        missing = page_ref.new_empty(1)
     _check(lib().sa_pages_reserve(
         _ptr(page_table), _ptr(seq_len), _ptr(page_ref), _ptr(n_new), B, max_pages,
         page_ref.numel(), int(page), _ptr(missing), _stream()))
@@ -568,13 +568,13 @@ def sa_pages_fork(page_table, seq_len, page_ref, src, dst, page, *, copy_src=Non
     for name, t in (("src", src), ("dst", dst), ("copy_src", copy_src), ("copy_dst", copy_dst)):
         _expect(t, name, (n,), torch.int32)
     _expect(missing, "missing", (1,), torch.int32)
-    dev = _here(page_table, seq_len, page_ref, src, dst, copy_src, copy_dst, missing)
+    _here(page_table, seq_len, page_ref, src, dst, copy_src, copy_dst, missing)
     if copy_src is None:
-        copy_src = torch.empty(n, dtype=torch.int32, device=dev)
+        copy_src = page_ref.new_empty(n)
     if copy_dst is None:
-        copy_dst = torch.empty(n, dtype=torch.int32, device=dev)
+        copy_dst = page_ref.new_empty(n)
     if missing is None:
-        missing = torch.empty(1, dtype=torch.int32, device=dev)
+        missing = page_ref.new_empty(1)
     _check(lib().sa_pages_fork(
         _ptr(page_table), _ptr(seq_len), _ptr(page_ref), _ptr(src), _ptr(dst), n, B, max_pages,
         page_ref.numel(), int(page), _ptr(copy_src), _ptr(copy_dst), _ptr(missing), _stream()))
@@ -601,13 +601,13 @@ def sa_pages_compact(page_table, page_ref, *, move_src=None, move_dst=None, coun
     _expect(move_src, "move_src", (n_pages // 2,), torch.int32)
     _expect(move_dst, "move_dst", (n_pages // 2,), torch.int32)
     _expect(counts, "counts", (2,), torch.int32)
-    dev = _here(page_table, page_ref, move_src, move_dst, counts)
+    _here(page_table, page_ref, move_src, move_dst, counts)
     if move_src is None:
-        move_src = torch.empty(n_pages // 2, dtype=torch.int32, device=dev)
+        move_src = page_ref.new_empty(n_pages // 2)
     if move_dst is None:
-        move_dst = torch.empty(n_pages // 2, dtype=torch.int32, device=dev)
+        move_dst = page_ref.new_empty(n_pages // 2)
     if counts is None:
-        counts = torch.empty(2, dtype=torch.int32, device=dev)
+        counts = page_ref.new_empty(2)
     _check(lib().sa_pages_compact(
         _ptr(page_table), _ptr(page_ref), B, max_pages, n_pages,
         _ptr(move_src) if n_pages > 1 else None, _ptr(move_dst) if n_pages > 1 else None,
@@ -657,7 +657,8 @@ def sa_prefix_attention(q, k_pages, v_pages, page_table, seq_len, scale, *, shar
     if shared_len is not None:
         n_groups = shared_len.numel()
         _expect(shared_len, "shared_len", (n_groups,), torch.int32)
-    dev = _here(q, k_pages, v_pages, page_table, seq_len, shared_len, q_len, o, lse, ws)
+    _here(q, k_pages, v_pages, page_table, seq_len, shared_len, q_len, o, lse, ws)
+    dev = q.device
     make = torch.empty if q_len is None else torch.zeros
     if o is None:
         o = make(B, Hq, S, d, dtype=q.dtype, device=dev)

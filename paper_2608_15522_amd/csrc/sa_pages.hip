@@ -15,98 +15,104 @@ namespace {
 constexpr int kScanThreads = 1024;
 constexpr int kScanWaves = kScanThreads / kWave;
 constexpr int kScanEach = 16;                           // pages per thread and step
+constexpr int kScanChunks = kScanWaves * kScanEach;     // chunks of 64 pages per step
 constexpr int kScanStep = kScanThreads * kScanEach;     // pages per step
+constexpr size_t kOnePass = 8192;  // table entries that a planning workgroup rewrites itself
 
 __device__ __forceinline__ int pages_of(long long tokens, int lp) {
   return static_cast<int>((tokens + (1ll << lp) - 1) >> lp);
 }
 
-// Page flags of one step, kept as the ballots of the wave's 16 loads (64 consecutive
-// pages each, so the loads are coalesced and a page's rank is a count of bits).
-// One workgroup takes 16384 pages a step: 64 bytes in flight a lane.
-struct PageFlags {
-  uint64_t m[kScanEach];
-  template <class F>
-  __device__ __forceinline__ void read(int p0, int n_pages, F flag) {
-    const int lane = threadIdx.x & 63;
-    bool f[kScanEach];
+// The planning kernels are one workgroup that looks through the owner counts, 16384 pages
+// a step, and numbers the pages of a kind in ascending order.  They are bound by latency
+// and by cold instruction fetches, so all loads of a step go out together and everything
+// else is rolled up: wave w holds chunks w, w + 16, ... of 64 consecutive pages, one bit a
+// lane and chunk, and a page's rank is a count of bits behind the sum of the chunks before.
+__device__ __forceinline__ int chunk_page(int p0, int j) {
+  return p0 + 64 * (j * kScanWaves + (static_cast<int>(threadIdx.x) >> 6)) +
+         (static_cast<int>(threadIdx.x) & 63);
+}
+template <class F>
+__device__ __forceinline__ uint32_t read_flags(int p0, int n_pages, F flag) {
+  uint32_t bits = 0;
 #pragma unroll
-    for (int j = 0; j < kScanEach; ++j) {
-      const int p = p0 + 64 * j + lane;
-      f[j] = p < n_pages && flag(p);
-    }
-#pragma unroll
-    for (int j = 0; j < kScanEach; ++j) m[j] = __ballot(f[j]);
+  for (int j = 0; j < kScanEach; ++j) {
+    const int p = chunk_page(p0, j);
+    if (p < n_pages && flag(p)) bits |= 1u << j;
   }
-  __device__ __forceinline__ int count() const {
-    int c = 0;
-#pragma unroll
-    for (int j = 0; j < kScanEach; ++j) c += __popcll(m[j]);
-    return c;
-  }
-  // f(page, rank) for each flagged page of the lane; rank counts from `before`.
-  template <class F>
-  __device__ __forceinline__ void each(int p0, int before, F f) const {
-    const int lane = threadIdx.x & 63;
-    const uint64_t below = (1ull << lane) - 1ull;
-#pragma unroll
-    for (int j = 0; j < kScanEach; ++j) {
-      if ((m[j] >> lane) & 1) f(p0 + 64 * j + lane, before + __popcll(m[j] & below));
-      before += __popcll(m[j]);
-    }
-  }
+  return bits;
+}
+// Counts the pages of a step whose bit is set and sums them up over the chunks: returns
+// their number.  Callers alternate between cnt's, so that one barrier a step is enough.
+struct Ranks {
+  int excl;  // lane l: pages in chunks before 4 l
 };
-
-// Sum over the waves of a workgroup-wide step: returns the total, `before` the part
-// of the waves in front of this one.  `slot` alternates so that one barrier is enough.
-__device__ __forceinline__ int step_total(int own, int slot, int (*tot)[kScanWaves], int* before) {
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  if (lane == 0) tot[slot][wave] = own;
-  __syncthreads();
-  int sum = 0, pre = 0;
-#pragma unroll
-  for (int w = 0; w < kScanWaves; ++w) {
-    const int v = tot[slot][w];
-    if (w < wave) pre += v;
-    sum += v;
+__device__ __forceinline__ int rank_flags(uint32_t bits, int* cnt, Ranks* r) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll 1
+  for (int j = 0; j < kScanEach; ++j) {
+    const int c = __popcll(__ballot((bits >> j) & 1));
+    if (lane == 0) cnt[j * kScanWaves + wave] = c;
   }
-  *before = pre;
-  return sum;
+  __syncthreads();
+  const int own = cnt[4 * lane] + cnt[4 * lane + 1] + cnt[4 * lane + 2] + cnt[4 * lane + 3];
+  int incl = own;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int u = __shfl_up(incl, o, 64);
+    if (lane >= o) incl += u;
+  }
+  r->excl = incl - own;
+  return __shfl(incl, 63, 64);
+}
+// f(page, rank) for every such page of the lane, ranks from `base` on.
+template <class F>
+__device__ __forceinline__ void take_flags(uint32_t bits, int p0, int base, const int* cnt,
+                                           const Ranks& r, F f) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll 1
+  for (int j = 0; j < kScanEach; ++j) {
+    const uint64_t b = __ballot((bits >> j) & 1);
+    if (b == 0) continue;
+    const int q = j * kScanWaves + wave;
+    int before = base + __shfl(r.excl, q >> 2, 64);
+    for (int k = q & ~3; k < q; ++k) before += cnt[k];
+    if ((b >> lane) & 1) f(chunk_page(p0, j), before + __popcll(b & ((1ull << lane) - 1ull)));
+  }
 }
 
-__device__ __forceinline__ int step_page(int p0) { return p0 + (threadIdx.x >> 6) * 64 * kScanEach; }
-
-// Free pages among the first ones that are needed: exact if fewer than `want`.
-__device__ int count_free(const int32_t* __restrict__ ref, int n_pages, long long want,
-                          int (*tot)[kScanWaves]) {
-  int found = 0, before;
-  for (int p0 = 0, k = 0; p0 < n_pages && found < want; p0 += kScanStep, ++k) {
-    PageFlags f;
-    f.read(step_page(p0), n_pages, [&](int p) { return ref[p] == 0; });
-    found += step_total(f.count(), k & 1, tot, &before);
-  }
-  __syncthreads();
+// Free pages among the first ones that are needed: exact if fewer than `want`.  `bits`
+// are the first step's flags, whose ranks are r0 and cnt[0], their number *first.
+__device__ int count_free(uint32_t bits, const int32_t* __restrict__ ref, int n_pages,
+                          long long want, int (*cnt)[kScanChunks], Ranks* r0, int* first) {
+  int found = *first = rank_flags(bits, cnt[0], r0);
+  Ranks r;
+  for (int p0 = kScanStep, k = 0; p0 < n_pages && found < want; p0 += kScanStep, ++k)
+    found += rank_flags(read_flags(p0, n_pages, [&](int p) { return ref[p] == 0; }),
+                        cnt[1 + (k & 1)], &r);
   return found;
 }
 
 // take(page, rank) for the `want` lowest free pages (there are so many), which get one
-// owner.
+// owner.  A barrier lies between count_free and this.
 template <class F>
-__device__ void take_free(int32_t* __restrict__ ref, int n_pages, int want,
-                          int (*tot)[kScanWaves], F take) {
+__device__ void take_free(uint32_t bits, Ranks r, int number, int32_t* __restrict__ ref,
+                          int n_pages, int want, int (*cnt)[kScanChunks], F take) {
+  const int* c = cnt[0];
   int base = 0;
-  for (int p0 = 0, k = 0; p0 < n_pages && base < want; p0 += kScanStep, ++k) {
-    PageFlags f;
-    f.read(step_page(p0), n_pages, [&](int p) { return ref[p] == 0; });
-    int before;
-    const int all = step_total(f.count(), k & 1, tot, &before);
-    f.each(step_page(p0), base + before, [&](int p, int rank) {
+  for (int p0 = 0, k = 0;; ++k) {
+    take_flags(bits, p0, base, c, r, [&](int p, int rank) {
       if (rank < want) {
         take(p, rank);
         ref[p] = 1;
       }
     });
-    base += all;
+    base += number;
+    p0 += kScanStep;
+    if (p0 >= n_pages || base >= want) return;
+    bits = read_flags(p0, n_pages, [&](int p) { return ref[p] == 0; });
+    c = cnt[1 + (k & 1)];
+    number = rank_flags(bits, cnt[1 + (k & 1)], &r);
   }
 }
 
@@ -139,37 +145,46 @@ __device__ __forceinline__ int2 reserve_span(const int32_t* __restrict__ seq_len
 }
 
 // One workgroup: the pages' order is a prefix sum over the sequences, then one over the
-// free pages.  Latency-bound (a few dependent loads and barriers).
+// free pages.  Latency-bound: the lengths and the first 16384 owner counts are read at
+// once, everything after that is LDS and barriers unless there are more pages.
 __global__ void __launch_bounds__(kScanThreads)
 pages_reserve_kernel(int32_t* __restrict__ table, int32_t* __restrict__ seq_len,
                      int32_t* __restrict__ ref, const int32_t* __restrict__ n_new, int B,
                      int max_pages, int n_pages, int lp, int32_t* __restrict__ missing) {
-  __shared__ int tot[2][kScanWaves];
+  __shared__ int cnt[3][kScanChunks];
   __shared__ long long wave_tot[kScanWaves];
-  __shared__ int ends[kMaxSequences];  // pages of the sequences up to and with b
+  __shared__ unsigned long long over_all;
+  __shared__ int ends[kMaxSequences];  // new pages of the sequences up to and with b
+  __shared__ int have[kMaxSequences];  // pages of b
   const int tid = threadIdx.x;
   const int each = ceil_div(B, kScanThreads);
   const int b0 = min(tid * each, B), b1 = min(b0 + each, B);
+  if (tid == 0) over_all = 0;
+  const uint32_t bits = read_flags(0, n_pages, [&](int p) { return ref[p] == 0; });
   long long own = 0, over = 0;
   for (int b = b0; b < b1; ++b) {
     const int2 s = reserve_span(seq_len, n_new, b, lp);
+    have[b] = s.x;
+    ends[b] = s.y - s.x;
     own += s.y - s.x;
     over += max(s.y - max_pages, 0);
   }
-  long long total, lacking;
+  long long total;
   long long at = scan_threads(own, wave_tot, &total) - own;
-  scan_threads(over, wave_tot, &lacking);
-  const int found = count_free(ref, n_pages, total, tot);
-  lacking += max(total - found, 0ll);
+  if (over > 0) atomicAdd(&over_all, static_cast<unsigned long long>(over));
+  Ranks r;
+  int first;
+  const int found = count_free(bits, ref, n_pages, total, cnt, &r, &first);  // a barrier
+  const long long lacking = static_cast<long long>(over_all) + max(total - found, 0ll);
   if (tid == 0) missing[0] = static_cast<int32_t>(min(lacking, 0x7fffffffll));
   if (lacking > 0) return;
   for (int b = b0; b < b1; ++b) {  // total <= n_pages: 32 bits
-    const int2 s = reserve_span(seq_len, n_new, b, lp);
-    at += s.y - s.x;
+    at += ends[b];
     ends[b] = static_cast<int>(at);
+    seq_len[b] = max(seq_len[b], 0) + max(n_new[b], 0);
   }
   __syncthreads();
-  take_free(ref, n_pages, static_cast<int>(total), tot, [&](int p, int rank) {
+  take_free(bits, r, first, ref, n_pages, static_cast<int>(total), cnt, [&](int p, int rank) {
     int lo = 0, hi = B - 1;  // the first b with ends[b] > rank
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
@@ -178,11 +193,9 @@ pages_reserve_kernel(int32_t* __restrict__ table, int32_t* __restrict__ seq_len,
       else
         lo = mid + 1;
     }
-    const int2 s = reserve_span(seq_len, n_new, lo, lp);
-    table[static_cast<size_t>(lo) * max_pages + s.y - (ends[lo] - rank)] = p;
+    const int begin = lo > 0 ? ends[lo - 1] : 0;
+    table[static_cast<size_t>(lo) * max_pages + have[lo] + rank - begin] = p;
   });
-  __syncthreads();
-  for (int b = b0; b < b1; ++b) seq_len[b] = max(seq_len[b], 0) + max(n_new[b], 0);
 }
 
 // Entries of a fork: src must hold tokens and dst none, so the two sets are disjoint;
@@ -192,64 +205,95 @@ __device__ __forceinline__ bool fork_able(const int32_t* __restrict__ seq_len, i
   return src >= 0 && src < B && dst >= 0 && dst < B && seq_len[src] > 0 && seq_len[dst] <= 0;
 }
 
+// dst's row is src's, with the fresh page in the place of the partial last one, and every
+// shared page gets an owner more: entry j of the row.
+__device__ __forceinline__ void fork_entry(int32_t* __restrict__ table, int32_t* __restrict__ ref,
+                                           int a, int b, int full, int fresh, int j, int max_pages,
+                                           int n_pages) {
+  int p = j == full ? fresh : -1;
+  if (j < full) {
+    p = table[static_cast<size_t>(a) * max_pages + j];
+    if (p >= 0 && p < n_pages) atomicAdd(ref + p, 1);
+  }
+  table[static_cast<size_t>(b) * max_pages + j] = p;
+}
+
 // Pass 1 (one workgroup): which entries count, and a fresh page for each partial last
-// page.  copy_src holds kNoFork for an entry that does not count.
+// page.  ROWS: the table rows too, else copy_src holds kNoFork for an entry that does not
+// count until pass 2 has read it.
 constexpr int kNoFork = -2;
+template <bool ROWS>
 __global__ void __launch_bounds__(kScanThreads)
-pages_fork_plan_kernel(const int32_t* __restrict__ table, const int32_t* __restrict__ seq_len,
+pages_fork_plan_kernel(int32_t* __restrict__ table, int32_t* __restrict__ seq_len,
                        int32_t* __restrict__ ref, const int32_t* __restrict__ src,
                        const int32_t* __restrict__ dst, int n, int B, int max_pages, int n_pages,
                        int lp, int32_t* __restrict__ copy_src, int32_t* __restrict__ copy_dst,
                        int32_t* __restrict__ missing) {
-  __shared__ int tot[2][kScanWaves];
+  __shared__ int cnt[3][kScanChunks];
   __shared__ long long wave_tot[kScanWaves];
-  __shared__ int first[kMaxSequences];  // first able entry of each dst; then entries by rank
+  __shared__ int first[kMaxSequences];  // first able entry of each dst
+  __shared__ int entry[kMaxSequences];  // entries by the rank of their fresh page
   const int tid = threadIdx.x;
+  const uint32_t bits = read_flags(0, n_pages, [&](int p) { return ref[p] == 0; });
   for (int b = tid; b < B; b += kScanThreads) first[b] = 0x7fffffff;
   __syncthreads();
-  for (int i = tid; i < n; i += kScanThreads)
-    if (fork_able(seq_len, src[i], dst[i], B)) atomicMin(&first[dst[i]], i);
-  __syncthreads();
-  const int each = ceil_div(n, kScanThreads);
+  const int each = ceil_div(n, kScanThreads);  // at most 16
   const int i0 = min(tid * each, n), i1 = min(i0 + each, n);
-  auto counts = [&](int i) {
-    return fork_able(seq_len, src[i], dst[i], B) && first[dst[i]] == i;
-  };
-  auto partial = [&](int i) { return (seq_len[src[i]] & ((1 << lp) - 1)) != 0; };
-  int own = 0;
-  for (int i = i0; i < i1; ++i) own += counts(i) && partial(i);
+  unsigned counts = 0, part = 0;  // of the thread's entries: those that count, with a partial page
+  for (int i = i0; i < i1; ++i)
+    if (fork_able(seq_len, src[i], dst[i], B)) {
+      counts |= 1u << (i - i0);
+      atomicMin(&first[dst[i]], i);
+    }
+  __syncthreads();
+  for (int i = i0; i < i1; ++i) {
+    if (!((counts >> (i - i0)) & 1)) continue;
+    if (first[dst[i]] != i)
+      counts &= ~(1u << (i - i0));
+    else if ((seq_len[src[i]] & ((1 << lp) - 1)) != 0)
+      part |= 1u << (i - i0);
+  }
+  const int own = __popc(part);
   long long total;
-  int rank = static_cast<int>(scan_threads(own, wave_tot, &total)) - own;
-  const int found = count_free(ref, n_pages, total, tot);
+  int rank = static_cast<int>(scan_threads(own, wave_tot, &total)) - own, number;
+  Ranks r;
+  const int found = count_free(bits, ref, n_pages, total, cnt, &r, &number);
   const int lacking = max(static_cast<int>(total) - found, 0);
   if (tid == 0) missing[0] = lacking;
   for (int i = i0; i < i1; ++i) {
-    int last = kNoFork;
-    if (lacking == 0 && counts(i)) {
+    int last = ROWS ? -1 : kNoFork;
+    if (lacking == 0 && ((counts >> (i - i0)) & 1)) {
       const int full = seq_len[src[i]] >> lp;
-      last = partial(i) && full < max_pages
-                 ? table[static_cast<size_t>(src[i]) * max_pages + full] : -1;
-      if (last < 0 && last != -1) last = -1;  // an entry that is no page: nothing to copy
+      const bool partial = (part >> (i - i0)) & 1;
+      last = partial && full < max_pages ? table[static_cast<size_t>(src[i]) * max_pages + full]
+                                         : -1;
+      last = max(last, -1);  // an entry that is no page: nothing to copy
+      if (partial) entry[rank++] = i;
     }
     copy_src[i] = last;
     copy_dst[i] = -1;
   }
   if (lacking > 0) return;
-  __syncthreads();  // every thread is done with `first`
-  // entries by the rank of their fresh page: total <= n <= B
-  int* entry = first;
-  uint64_t mine = 0;  // each <= 16: the thread's entries that need one
-  for (int i = i0; i < i1; ++i)
-    if (copy_src[i] != kNoFork && partial(i)) mine |= 1ull << (i - i0);
-  for (int i = i0; i < i1; ++i)
-    if ((mine >> (i - i0)) & 1) entry[rank++] = i;
   __syncthreads();
-  take_free(ref, n_pages, static_cast<int>(total), tot,
-            [&](int p, int r) { copy_dst[entry[r]] = p; });
+  take_free(bits, r, number, ref, n_pages, static_cast<int>(total), cnt,
+            [&](int p, int k) { copy_dst[entry[k]] = p; });
+  if constexpr (ROWS) {
+    __syncthreads();  // the fresh pages are visible, and have their owner
+    for (int i = tid; i < n; i += kScanThreads) entry[i] = copy_dst[i];
+    __syncthreads();
+    // a row a wave
+    for (int i = tid >> 6; i < n; i += kScanWaves) {
+      const int a = src[i], b = dst[i];
+      if (b < 0 || b >= B || first[b] != i) continue;
+      const int full = seq_len[a] >> lp;
+      for (int j = tid & 63; j < max_pages; j += 64)
+        fork_entry(table, ref, a, b, full, entry[i], j, max_pages, n_pages);
+      if ((tid & 63) == 0) seq_len[b] = seq_len[a];
+    }
+  }
 }
 
-// Pass 2 (one workgroup an entry): dst's row is src's, with the fresh page in the place
-// of the partial last one, and every shared page gets an owner more.
+// Pass 2 (one workgroup an entry).
 __global__ void __launch_bounds__(256)
 pages_fork_kernel(int32_t* __restrict__ table, int32_t* __restrict__ seq_len,
                   int32_t* __restrict__ ref, const int32_t* __restrict__ src,
@@ -262,17 +306,9 @@ pages_fork_kernel(int32_t* __restrict__ table, int32_t* __restrict__ seq_len,
     if (tid == 0) copy_src[i] = -1;
     return;
   }
-  const int a = src[i], len = seq_len[a], full = len >> lp;
-  const int32_t* from = table + static_cast<size_t>(a) * max_pages;
-  int32_t* to = table + static_cast<size_t>(dst[i]) * max_pages;
-  for (int j = tid; j < max_pages; j += 256) {
-    int p = j == full ? fresh : -1;
-    if (j < full) {
-      p = from[j];
-      if (p >= 0 && p < n_pages) atomicAdd(ref + p, 1);
-    }
-    to[j] = p;
-  }
+  const int a = src[i], len = seq_len[a];
+  for (int j = tid; j < max_pages; j += 256)
+    fork_entry(table, ref, a, dst[i], len >> lp, fresh, j, max_pages, n_pages);
   if (tid == 0) seq_len[dst[i]] = len;
 }
 
@@ -300,51 +336,67 @@ pages_free_kernel(int32_t* __restrict__ table, int32_t* __restrict__ seq_len,
 }
 
 // Pass 1 (one workgroup): with U pages in use, the k-th used page from number U on
-// moves to the k-th free page below U.
+// moves to the k-th free page below U.  `entries` > 0 (with at most kScanStep pages): the
+// owners and the table too, through a map in LDS.
 __global__ void __launch_bounds__(kScanThreads)
-pages_compact_plan_kernel(const int32_t* __restrict__ ref, int n_pages,
-                          int32_t* __restrict__ move_src, int32_t* __restrict__ move_dst,
-                          int32_t* __restrict__ counts) {
-  __shared__ int tot[2][kScanWaves];
-  int used = 0, before;
-  for (int p0 = 0, k = 0; p0 < n_pages; p0 += kScanStep, ++k) {
-    PageFlags f;
-    f.read(step_page(p0), n_pages, [&](int p) { return ref[p] > 0; });
-    used += step_total(f.count(), k & 1, tot, &before);
-  }
-  __syncthreads();
+pages_compact_plan_kernel(int32_t* __restrict__ table, int32_t* __restrict__ ref, int entries,
+                          int n_pages, int32_t* __restrict__ move_src,
+                          int32_t* __restrict__ move_dst, int32_t* __restrict__ counts) {
+  __shared__ int cnt[4][kScanChunks];
+  __shared__ uint16_t rank_of[kScanStep];    // of a moved page; 0xffff: not moved
+  __shared__ uint16_t to[kScanStep / 2];     // place of the k-th moved page
+  auto in_use = [&](int p) { return ref[p] > 0; };
+  const int tid = threadIdx.x;
+  uint32_t bits = read_flags(0, n_pages, in_use);
+  if (entries > 0)
+    for (int p = tid; p < n_pages; p += kScanThreads) rank_of[p] = 0xffff;
+  Ranks r;
+  int used = rank_flags(bits, cnt[0], &r);
+  for (int p0 = kScanStep, k = 1; p0 < n_pages; p0 += kScanStep, ++k)
+    used += rank_flags(read_flags(p0, n_pages, in_use), cnt[k & 1], &r);
   int holes = 0, high = 0;
-  for (int p0 = 0, k = 0; p0 < n_pages; p0 += kScanStep, ++k) {
-    // a step may hold both: free pages below `used`, used ones from there on
-    PageFlags f;
-    f.read(step_page(p0), n_pages, [&](int p) { return (ref[p] > 0) == (p >= used); });
-    PageFlags g = f;
-    const int w0 = step_page(p0);
+  for (int p0 = 0, k = 0; p0 < n_pages; p0 += kScanStep, k ^= 1) {
+    // free pages below `used`, and used ones from there on; a step may hold both
+    if (p0 > 0) bits = read_flags(p0, n_pages, in_use);
+    uint32_t below = 0;
 #pragma unroll
-    for (int j = 0; j < kScanEach; ++j) {
-      const int first = w0 + 64 * j;  // bits of pages below `used`
-      const int n = used - first;
-      const uint64_t low = n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull;
-      f.m[j] &= low;
-      g.m[j] &= ~low;
-    }
-    const int a = step_total(f.count(), 0, tot, &before);
-    f.each(w0, holes + before, [&](int p, int r) { move_dst[r] = p; });
+    for (int j = 0; j < kScanEach; ++j) below |= chunk_page(p0, j) < used ? 1u << j : 0u;
+    const uint32_t hole = ~bits & below, move = bits & ~below;
+    int* c = cnt[2 + k];
+    const int a = rank_flags(hole, c, &r);
+    take_flags(hole, p0, holes, c, r, [&](int p, int i) {
+      move_dst[i] = p;
+      if (entries > 0) to[i] = static_cast<uint16_t>(p);
+    });
     holes += a;
-    const int c = step_total(g.count(), 1, tot, &before);
-    g.each(w0, high + before, [&](int p, int r) { move_src[r] = p; });
-    high += c;
+    c = cnt[k];
+    const int m = rank_flags(move, c, &r);
+    take_flags(move, p0, high, c, r, [&](int p, int i) {
+      move_src[i] = p;
+      if (entries > 0) rank_of[p] = static_cast<uint16_t>(i);
+    });
+    high += m;
   }
-  for (int r = high + threadIdx.x; r < n_pages / 2; r += kScanThreads)
-    move_src[r] = move_dst[r] = -1;
-  if (threadIdx.x == 0) {
+  for (int i = high + tid; i < n_pages / 2; i += kScanThreads) move_src[i] = move_dst[i] = -1;
+  if (tid == 0) {
     counts[0] = used;
     counts[1] = high;
   }
+  if (entries == 0) return;
+  __syncthreads();
+  for (int p = used + tid; p < n_pages; p += kScanThreads)
+    if (rank_of[p] != 0xffff) {
+      ref[to[rank_of[p]]] = ref[p];
+      ref[p] = 0;
+    }
+  for (int i = tid; i < entries; i += kScanThreads) {
+    const int p = table[i];
+    if (p >= used && p < n_pages && rank_of[p] != 0xffff) table[i] = to[rank_of[p]];
+  }
 }
 
-// Pass 2: table entries of moved pages (found in the ascending move_src by halving),
-// and the owners' counts.
+// Pass 2: table entries of moved pages (found in the ascending move_src by halving), and
+// the owners' counts.
 __global__ void __launch_bounds__(256)
 pages_compact_kernel(int32_t* __restrict__ table, int32_t* __restrict__ ref, size_t entries,
                      int n_pages, const int32_t* __restrict__ move_src,
@@ -461,9 +513,16 @@ void launch_pages_reserve(int32_t* table, int32_t* seq_len, int32_t* ref, const 
 void launch_pages_fork(int32_t* table, int32_t* seq_len, int32_t* ref, const int32_t* src,
                        const int32_t* dst, int n, int B, int max_pages, int n_pages, int page,
                        int32_t* copy_src, int32_t* copy_dst, int32_t* missing, hipStream_t s) {
-  hipLaunchKernelGGL(pages_fork_plan_kernel, dim3(1), dim3(kScanThreads), 0, s, table, seq_len,
-                     ref, src, dst, n, B, max_pages, n_pages, log2_of(page), copy_src, copy_dst,
-                     missing);
+  // rows of few entries are written by the planning workgroup, which saves a launch
+  if (static_cast<size_t>(n) * max_pages <= kOnePass) {
+    hipLaunchKernelGGL(pages_fork_plan_kernel<true>, dim3(1), dim3(kScanThreads), 0, s, table,
+                       seq_len, ref, src, dst, n, B, max_pages, n_pages, log2_of(page), copy_src,
+                       copy_dst, missing);
+    return;
+  }
+  hipLaunchKernelGGL(pages_fork_plan_kernel<false>, dim3(1), dim3(kScanThreads), 0, s, table,
+                     seq_len, ref, src, dst, n, B, max_pages, n_pages, log2_of(page), copy_src,
+                     copy_dst, missing);
   hipLaunchKernelGGL(pages_fork_kernel, dim3(n), dim3(256), 0, s, table, seq_len, ref, src, dst,
                      max_pages, n_pages, log2_of(page), copy_src, copy_dst);
 }
@@ -476,9 +535,11 @@ void launch_pages_free(int32_t* table, int32_t* seq_len, int32_t* ref, const int
 
 void launch_pages_compact(int32_t* table, int32_t* ref, int B, int max_pages, int n_pages,
                           int32_t* move_src, int32_t* move_dst, int32_t* counts, hipStream_t s) {
-  hipLaunchKernelGGL(pages_compact_plan_kernel, dim3(1), dim3(kScanThreads), 0, s, ref, n_pages,
-                     move_src, move_dst, counts);
   const size_t entries = static_cast<size_t>(B) * max_pages;
+  const bool one = entries <= kOnePass && n_pages <= kScanStep;
+  hipLaunchKernelGGL(pages_compact_plan_kernel, dim3(1), dim3(kScanThreads), 0, s, table, ref,
+                     one ? static_cast<int>(entries) : 0, n_pages, move_src, move_dst, counts);
+  if (one) return;
   const size_t most = entries > static_cast<size_t>(n_pages) / 2 ? entries : n_pages / 2 + 1;
   const size_t wgs = (most + 255) / 256;
   hipLaunchKernelGGL(pages_compact_kernel, dim3(static_cast<unsigned>(wgs < 2048 ? wgs : 2048)),
