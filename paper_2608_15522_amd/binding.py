@@ -10,6 +10,7 @@ arithmetic runs in the library's kernels.  There is no fallback: if
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional
 
@@ -631,6 +632,7 @@ def sa_pages_copy(pools, src, dst):
     return pools
 
 
+@functools.lru_cache(maxsize=256)
 def sa_prefix_attention_workspace(B: int, Hq: int, Hkv: int, S: int, d: int, dtype,
                                   n_groups: int = 0) -> int:
     """Workspace bytes of sa_prefix_attention."""
