@@ -31,8 +31,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4_t;
 
 constexpr int kTile = 64;         // keys per unit of work
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / kWave;
+constexpr int kMaxWaves = 8;      // waves of a workgroup: 4, or 8 of the forms of few rows
 constexpr int kSegs = kMaxAttendSegs;
 
 // The running max is raised when a score exceeds it by 2^8, as in the other attention
@@ -103,7 +102,7 @@ __device__ __forceinline__ int div_small(int x, int y, float inv) {
 // (causal) what its first query sees.
 struct Schedule {
   int off[kSegs + 1];
-  int wave_tot[kWaves];
+  int wave_tot[kMaxWaves];
   int len[kSegs];
   int sh[kSegs / 2];
   int most;  // units of the longest row tile
@@ -116,12 +115,14 @@ __device__ __forceinline__ int row_units(const Cost& c, int keys) {
   return c.row + c.tile * ceil_div(keys, kTile);
 }
 
+template <int W>
 __device__ void build_schedule(const Args& a, Schedule& s) {
+  constexpr int NT = W * kWave;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  for (int g = tid; g < a.G; g += kThreads) s.sh[g] = 0x7fffffff;
+  for (int g = tid; g < a.G; g += NT) s.sh[g] = 0x7fffffff;
   if (tid == 0) s.most = 0;
   __syncthreads();
-  for (int b = tid; b < a.B; b += kThreads) {
+  for (int b = tid; b < a.B; b += NT) {
     const int len = seq_tokens(a, b);
     s.len[b] = len;
     if (a.G == 0) atomicMax(&s.most, row_units(a.co, len));
@@ -130,14 +131,14 @@ __device__ void build_schedule(const Args& a, Schedule& s) {
   }
   __syncthreads();
   if (a.G > 0) {
-    for (int g = tid; g < a.G; g += kThreads) {
+    for (int g = tid; g < a.G; g += NT) {
       // no sequence of the group has a key: nothing to share
       const int v = s.sh[g] == 0x7fffffff ? 0 : min(s.sh[g], max(a.shared_len[g], 0));
       s.sh[g] = v >> a.lp << a.lp;
     }
     __syncthreads();
   }
-  const int n = a.G + a.B, each = ceil_div(n, kThreads);
+  const int n = a.G + a.B, each = ceil_div(n, NT);
   const int i0 = min(tid * each, n), i1 = min(i0 + each, n);
   auto units = [&](int i) {
     if (i < a.G) return s.sh[i] == 0 ? 0 : a.nrtp * row_units(a.cp, s.sh[i]);
@@ -156,7 +157,7 @@ __device__ void build_schedule(const Args& a, Schedule& s) {
   __syncthreads();
   int at = incl - sum;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w)
+  for (int w = 0; w < W; ++w)
     if (w < wave) at += s.wave_tot[w];
   for (int i = i0; i < i1; ++i) {
     s.off[i] = at;
@@ -303,29 +304,29 @@ __device__ __forceinline__ void put_row(const Args& a, const Job& j, int jr, int
 }
 
 // Joins the waves' partial rows of a row tile, in wave order.  A wave's rows lie in its
-// own LDS buffers (W bytes each), slot c4 of row r at join_slot(r, c4).
+// own LDS buffers (BYTES each), slot c4 of row r at join_slot(r, c4).
 constexpr int kJoinRows = 32;
 template <int D>
 __device__ __forceinline__ int join_slot(int r, int c4) {
   return r * D * 4 + ((c4 ^ r) & (D / 4 - 1)) * 16;
 }
-template <int D, int W, typename T>
+template <int D, int W, int BYTES, typename T>
 __device__ __forceinline__ void join_waves(const Args& a, const Job& j, int rows,
                                            const char* lds_all, const float2* lds_ml) {
   __syncthreads();
   constexpr int TPR = D / 4;
-  for (int u = threadIdx.x; u < rows * TPR; u += kThreads) {
+  for (int u = threadIdx.x; u < rows * TPR; u += W * kWave) {
     const int jr = u / TPR, c4 = u % TPR;
     float M = -FLT_MAX, den = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w)
+    for (int w = 0; w < W; ++w)
       if (lds_ml[w * kJoinRows + jr].y != 0.f) M = fmaxf(M, lds_ml[w * kJoinRows + jr].x);
     f32x4 num = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < W; ++w) {
       const float2 ml = lds_ml[w * kJoinRows + jr];
       const float f = ml.y != 0.f ? fast_exp2(ml.x - M) : 0.f;
-      const f32x4 x = *reinterpret_cast<const f32x4*>(lds_all + w * W + join_slot<D>(jr, c4));
+      const f32x4 x = *reinterpret_cast<const f32x4*>(lds_all + w * BYTES + join_slot<D>(jr, c4));
       den = fmaf(f, ml.y, den);
 #pragma unroll
       for (int e = 0; e < 4; ++e) num[e] = fmaf(f, x[e], num[e]);
@@ -361,7 +362,7 @@ __device__ __forceinline__ void lds_dma16_once(const char* sbase, uint32_t voff,
       : "v"(voff), "s"(sbase), "s"(lds_addr)
       : "memory", "m0");
 }
-template <int D>
+template <int D, int W>
 __device__ void attend_few(const Args& a, const Job& j, char* lds_all, float2* lds_ml) {
   constexpr int KC = D / 16, DT = D / 32, NI = kPiece * D * 2 / 1024;
   constexpr int BUF = kPiece * D * 2;  // bytes
@@ -431,8 +432,8 @@ __device__ void attend_few(const Args& a, const Job& j, char* lds_all, float2* l
     issue(a.kp, lds_k);
     issue(a.vp, lds_v);
   }
-  for (int pos = first; pos < run1; pos += kPiece * kWaves) {
-    const bool more = pos + kPiece * kWaves < run1;
+  for (int pos = first; pos < run1; pos += kPiece * W) {
+    const bool more = pos + kPiece * W < run1;
     const bool masked = bad || pos + kPiece > run1 || (a.causal && !j.shared);
     wait_vm<NI>();  // K; V's copies are behind it
     __builtin_amdgcn_sched_barrier(0);
@@ -446,7 +447,7 @@ __device__ void attend_few(const Args& a, const Job& j, char* lds_all, float2* l
     wait_lds();  // the reads of K are done
     __builtin_amdgcn_sched_barrier(0);
     if (more) {
-      look(pos + kPiece * kWaves);
+      look(pos + kPiece * W);
       issue(a.kp, lds_k);
     }
     bool none[2] = {false, false};  // the piece's 16-key groups without a page
@@ -536,7 +537,7 @@ __device__ void attend_few(const Args& a, const Job& j, char* lds_all, float2* l
             f32x4{acc[dt][4 * rg], acc[dt][4 * rg + 1], acc[dt][4 * rg + 2], acc[dt][4 * rg + 3]};
     if (g == 0) lds_ml[wave * kJoinRows + n] = make_float2(m, ltot);
   }
-  join_waves<D, 2 * BUF, uint16_t>(a, j, rows, lds_all, lds_ml);
+  join_waves<D, W, 2 * BUF, uint16_t>(a, j, rows, lds_all, lds_ml);
 }
 
 // ---- bf16, many rows --------------------------------------------------------------------
@@ -905,7 +906,7 @@ __device__ void attend_many(const Args& a, const Job& j, char* lds) {
 //                  tile (dq, e) for channel 64dq + 4i + e.
 // Weights are taken down by 2^-8, the slack of the running max, so that none exceeds 1.
 constexpr int kF32Keys = 16;
-template <int D>
+template <int D, int W>
 __device__ void attend_f32(const Args& a, const Job& j, char* lds_all, float2* lds_ml) {
   constexpr int KI = D / 16, DQ = D / 64;
   using KTile = RowTile16<D>;
@@ -945,7 +946,7 @@ __device__ void attend_f32(const Args& a, const Job& j, char* lds_all, float2* l
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[dq][e] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = -FLT_MAX, lsum = 0.f;
-  constexpr int STEP = kF32Keys * kWaves;
+  constexpr int STEP = kF32Keys * W;
   auto step = [&](int pos, int buf, Piece& x, Piece& nx) {
     wait_dma();
     __builtin_amdgcn_sched_barrier(0);
@@ -1026,13 +1027,13 @@ __device__ void attend_f32(const Args& a, const Job& j, char* lds_all, float2* l
     // 2^-8 goes back into the reference, exactly
     if (gk == 0) lds_ml[wave * kJoinRows + n] = make_float2(m + kRescaleSlack, lsum);
   }
-  join_waves<D, 2 * KTile::kBytes, float>(a, j, rows, lds_all, lds_ml);
+  join_waves<D, W, 2 * KTile::kBytes, float>(a, j, rows, lds_all, lds_ml);
 }
 
 // Bytes of LDS that the waves' buffers take: 16 KB a wave at d = 128 for either type.
-template <int D>
+template <int D, int W>
 constexpr int attend_lds() {
-  return kWaves * 128 * D;
+  return W * 128 * D;
 }
 
 // ---- the runs ---------------------------------------------------------------------------
@@ -1095,11 +1096,14 @@ __device__ __forceinline__ Tile tile_of(const Args& a, int t) {
   return x;
 }
 
-template <int D, typename T, bool MANY_SHARED, bool MANY_OWN>
-__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
+// W waves a workgroup: with eight, two workgroups' worth of buffers and waves work on one
+// row tile.
+template <int D, typename T, bool MANY_SHARED, bool MANY_OWN, int W>
+__global__ void __launch_bounds__(W * kWave) __attribute__((amdgpu_waves_per_eu(2, 2)))
 prefix_attention_kernel(const Args a, Split split) {
-  __shared__ __attribute__((aligned(1024))) char lds[attend_lds<D>()];
-  __shared__ float2 lds_ml[kWaves * kJoinRows];
+  static_assert(W == 4 || !(MANY_SHARED || MANY_OWN), "the form of many rows has four waves");
+  __shared__ __attribute__((aligned(1024))) char lds[attend_lds<D, W>()];
+  __shared__ float2 lds_ml[W * kJoinRows];
   __shared__ Schedule s;
   const int lane = threadIdx.x & 63;
   const int xcd = blockIdx.x & 7, in_xcd = blockIdx.x >> 3, slots_xcd = gridDim.x >> 3;
@@ -1111,13 +1115,13 @@ prefix_attention_kernel(const Args a, Split split) {
   int per_head = 1, total = 0;
   float inv_head = 1.f;
   if (!whole) {
-    build_schedule(a, s);
+    build_schedule<W>(a, s);
     per_head = uniform(s.off[a.G + a.B]);
     total = per_head * a.Hkv;
     inv_head = 1.f / static_cast<float>(per_head);
     if (blockIdx.x == 0)
-      for (int i = threadIdx.x; i < a.G; i += kThreads) a.shared_out[i] = s.sh[i];
-    rounds = a.G == 0 && nt >= kPrefixSlots &&
+      for (int i = threadIdx.x; i < a.G; i += W * kWave) a.shared_out[i] = s.sh[i];
+    rounds = a.G == 0 && nt >= static_cast<int>(gridDim.x) &&
              uniform(s.most) <= 1.25f * static_cast<float>(total) / static_cast<float>(nt);
   }
   // Rounds: row tiles [t, end) of the XCD, slots_xcd at a time.  What remains then, less than
@@ -1141,7 +1145,7 @@ prefix_attention_kernel(const Args a, Split split) {
   }
   // The run: units [u, stop) of the call or, after the rounds, of the XCD's rest.
   const int my = rounds ? in_xcd : slot;
-  const int run = whole ? 1 : run_units(total, rounds ? slots_xcd : kPrefixSlots);
+  const int run = whole ? 1 : run_units(total, rounds ? slots_xcd : gridDim.x);
   auto place = [&](int x) {
     if (!rounds) return place_of(a, s, per_head, inv_head, x);
     Place p;
@@ -1216,17 +1220,17 @@ prefix_attention_kernel(const Args a, Split split) {
     if (!whole && p.k == 0 && threadIdx.x == 0)
       a.parts[tile] = make_int2(slot, j.pos1 == j.pos0 ? 0 : last + 1);
     if constexpr (sizeof(T) == 4) {
-      attend_f32<D>(a, j, lds, lds_ml);
+      attend_f32<D, W>(a, j, lds, lds_ml);
     } else if constexpr (MANY_SHARED == MANY_OWN) {
       if constexpr (MANY_OWN)
         attend_many<D>(a, j, lds);
       else
-        attend_few<D>(a, j, lds, lds_ml);
+        attend_few<D, W>(a, j, lds, lds_ml);
     } else {
       if (j.shared)
         attend_many<D>(a, j, lds);
       else
-        attend_few<D>(a, j, lds, lds_ml);
+        attend_few<D, W>(a, j, lds, lds_ml);
     }
   }
 }
@@ -1316,23 +1320,58 @@ prefix_combine_kernel(const Args a, int chunk) {
   }
 }
 
-// Whether every row tile goes to a workgroup of its own, which saves finding the runs and
-// the joining kernel (some 6 us), by the keys that a table row has room for.  One workgroup
-// takes 4 to 6 us a thousand keys, so up to 1024 keys it is as fast as runs however few the
-// row tiles: 24 heads of 2 sequences (48 row tiles) at d 128 take 16.1 against 21.4 us with
-// room for 1000 keys, 27.5 against 23.6 with room for 2000; with at least as many row tiles
-// as slots up to 2048 (720 row tiles: 86 against 89 us; 162 against 150 for 4000); and with
-// eight times as many at any length, since these even out by themselves (4800 row tiles,
-// 1000 keys: 230 against 255 us).  Under a causal mask the row tiles of a sequence whose
-// queries are a quarter of its tokens or more see unequally many keys, which runs do not
-// know: as many row tiles as slots suffice (528 of up to 1700 keys: 51 against 62 us).  Where sequences share tokens, reading these once for all is given up only
-// for so few keys that the L2 makes up for it.
-bool whole_tiles(const Args& a, const PrefixCall& p) {
+// How a call is cut up, by its row tiles and by the keys that a table row has room for.
+// Every row tile whole, in a workgroup of its own, saves finding the runs and the joining
+// kernel (some 5 us); a workgroup of eight waves reads one row tile's keys at twice the rate
+// of one of four, where there is a CU for each.  Timed over 4 to 800 row tiles of sequences
+// of 1 to 4000 tokens (us; whole with 4 waves, runs with 4, whole with 8, runs with 8):
+//   bf16, d 128,  24 row tiles, up to 1000 keys  13.8  20.3  12.6  17.3
+//                                  4000          42.0  21.3  28.9  19.8
+//                256               1000          17.8  26.1  18.1  27.1
+//                512               1000          29.6  38.4  32.4  39.1
+//                                  2000          65.7  67.9  64.9  63.1
+//   bf16, d 64,  128               2000          19.8  20.0  14.1  20.2
+//                512               2000          26.9  35.2  28.4  38.3
+//   fp32, d 128,  24               1000          24.7  28.3  24.1  21.8
+//                512               4000         217.7 197.4 203.8 193.0
+struct Plan {
+  Split split;
+  int waves;
+};
+Plan plan_of(const Args& a, const PrefixCall& p, bool bf16, int d) {
+  const bool many_own = a.TRo == kManyRows, many = many_own || (a.G > 0 && a.TRp == kManyRows);
   const long long tiles = static_cast<long long>(a.Hkv) * a.B * a.nrto;
   const long long keys = static_cast<long long>(p.max_pages) * p.page;
-  if (a.G > 0) return keys <= 1024 && tiles * keys <= 1 << 17;
-  return keys <= 1024 || (tiles >= kPrefixSlots && (keys <= 2048 || (p.causal && keys <= 4ll * p.S))) ||
-         tiles >= 8 * kPrefixSlots;
+  const int row = d * (bf16 ? 2 : 4);
+  bool whole;
+  if (a.G > 0) {
+    // reading shared tokens for each sequence: only for so few keys that the caches make up
+    // for it.  8 key heads, whole against shared: 64 sequences of 960 + up to 900 tokens at
+    // d 128 35 against 49 us, of 1920 + up to 900 45 against 50, of 3840 + up to 64 47 against
+    // 32; with 24 key heads 114 against 93, 146 against 96 and 133 against 44.
+    whole = bf16 ? keys <= 2048 && tiles * keys <= 1 << 20
+                 : keys * d <= 1 << 17 && tiles * keys * d <= 1 << 25;
+  } else if (many_own) {
+    // 48 row tiles of 144 rows at d 128: 16 against 21 us with room for 1000 keys, 27 against
+    // 24 with room for 2000.  Under a causal mask the row tiles of a sequence whose queries
+    // are a quarter of its tokens or more see unequally many keys, which runs do not know: as
+    // many row tiles as slots suffice (528 of up to 1700 keys: 51 against 62 us).
+    whole = keys <= 1024 ||
+            (tiles >= kPrefixSlots && (keys <= 2048 || (p.causal && keys <= 4ll * p.S)));
+  } else if (tiles <= kPrefixSlots / 2) {
+    whole = bf16 ? keys <= 2048 : keys * d <= 1 << 16;
+  } else {
+    whole = keys <= (row < 256 ? 2048 : 1024);
+  }
+  // with eight times as many row tiles as slots these even out by themselves
+  whole = whole || (a.G == 0 && tiles >= 8 * kPrefixSlots);
+  // workgroups without 128-row tiles have eight waves: whole row tiles while there is a CU for
+  // each, runs but for many row tiles of short rows or few keys
+  const bool few = !many || (whole && !many_own);
+  const bool eight =
+      few && (whole ? tiles <= kPrefixSlots / 2
+                    : tiles <= 64 || (row >= 256 && (tiles <= kPrefixSlots / 2 || keys > 1024)));
+  return {whole ? kWhole : kRuns, eight ? 8 : 4};
 }
 
 }  // namespace
@@ -1383,31 +1422,38 @@ void launch_prefix_attention(const PrefixCall& p, int dtype, int d, char* ws, hi
   const int at_once = kCombineThreads / (d / 4) / (share ? 8 : 1);
   const int chunk = a.G == 0 && !share ? (a.TRo < 32 ? a.TRo : 32) : at_once;
   const dim3 cgrid(ceil_div(a.RS, chunk), a.Hkv, a.B);
-  const Split split = whole_tiles(a, p) ? kWhole : kRuns;
+  const Plan plan = plan_of(a, p, dtype == 0, d);
+  const Split split = plan.split;
+  const bool wide = plan.waves == 8;
   if (split == kWhole) a.G = 0;
-  const int wgs = split == kWhole ? kXcds * ceil_div(a.Hkv * a.B * a.nrto, kXcds) : kPrefixSlots;
-#define SA_PREFIX(D, T, P, O)                                                                  \
-  do {                                                                                         \
-    hipLaunchKernelGGL((prefix_attention_kernel<D, T, P, O>), dim3(wgs), dim3(kThreads), 0, s, a, \
-                       split);                                                                 \
-    if (split == kWhole) break;                                                                \
-    if (share)                                                                                 \
-      hipLaunchKernelGGL((prefix_combine_kernel<D, T, 8>), cgrid, dim3(kCombineThreads), 0, s, a, \
-                         chunk);                                                               \
-    else                                                                                       \
-      hipLaunchKernelGGL((prefix_combine_kernel<D, T, 1>), cgrid, dim3(kCombineThreads), 0, s, a, \
-                         chunk);                                                               \
+  const int slots = wide ? kPrefixSlots / 2 : kPrefixSlots;
+  const int wgs = split == kWhole ? kXcds * ceil_div(a.Hkv * a.B * a.nrto, kXcds) : slots;
+#define SA_PREFIX(D, T, P, O, W)                                                              \
+  do {                                                                                        \
+    hipLaunchKernelGGL((prefix_attention_kernel<D, T, P, O, W>), dim3(wgs), dim3(W * kWave), 0, \
+                       s, a, split);                                                          \
+    if (split == kWhole) break;                                                               \
+    if (share)                                                                                \
+      hipLaunchKernelGGL((prefix_combine_kernel<D, T, 8>), cgrid, dim3(kCombineThreads), 0, s, \
+                         a, chunk);                                                           \
+    else                                                                                      \
+      hipLaunchKernelGGL((prefix_combine_kernel<D, T, 1>), cgrid, dim3(kCombineThreads), 0, s, \
+                         a, chunk);                                                           \
   } while (0)
-#define SA_PREFIX_D(D)                        \
-  do {                                        \
-    if (dtype != 0)                           \
-      SA_PREFIX(D, float, false, false);      \
-    else if (a.TRo == kManyRows)              \
-      SA_PREFIX(D, uint16_t, true, true);     \
-    else if (a.TRp == kManyRows)              \
-      SA_PREFIX(D, uint16_t, true, false);    \
-    else                                      \
-      SA_PREFIX(D, uint16_t, false, false);   \
+#define SA_PREFIX_D(D)                          \
+  do {                                          \
+    if (dtype != 0 && wide)                     \
+      SA_PREFIX(D, float, false, false, 8);     \
+    else if (dtype != 0)                        \
+      SA_PREFIX(D, float, false, false, 4);     \
+    else if (wide)                              \
+      SA_PREFIX(D, uint16_t, false, false, 8);  \
+    else if (a.TRo == kManyRows)                \
+      SA_PREFIX(D, uint16_t, true, true, 4);    \
+    else if (a.TRp == kManyRows && a.G > 0)     \
+      SA_PREFIX(D, uint16_t, true, false, 4);   \
+    else                                        \
+      SA_PREFIX(D, uint16_t, false, false, 4);  \
   } while (0)
   if (d == 128)
     SA_PREFIX_D(128);
