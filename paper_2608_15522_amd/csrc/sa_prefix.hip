@@ -39,15 +39,12 @@ constexpr int kSegs = kMaxAttendSegs;
 constexpr float kRescaleSlack = 8.0f;
 constexpr float kSlackWeight = 1.f / 256.f;  // 2^-kRescaleSlack
 
-// Units of work of a row tile: `row` for what it costs whatever its keys (finding its
-// pages, the first copies' latency, its epilogue), `tile` for each 64-key tile.  A cut
+// Units of work of a row tile: one for each 64-key tile, and `cost` for what it takes
+// whatever its keys (finding its pages, the first copies' latency, its epilogue).  A cut
 // leaves at least kSnap tiles on either side, or moves to the row tile's end.  64 samples
 // of 4 query heads a key head (8 of them) over 16384 shared tokens and up to 2000 of their
-// own at d 128 take 113 us with row costs of 4 (128 rows) and 6 (32 rows) and equal tiles,
-// 125 to 131 with tiles of the 32-row form at twice the other's, 114 the other way round.
-struct Cost {
-  int row, tile;
-};
+// own at d 128 take 113 us with costs of 4 (128 rows) and 6 (32 rows), 125 to 131 with tiles
+// of the 32-row form at twice the other's, 114 the other way round.
 constexpr int kSnap = 2;
 constexpr int kRunMin = 5;  // least units of a run
 
@@ -63,14 +60,16 @@ struct Args {
   const int32_t* q_len;       // NULL: S queries each
   int B, G, N;                // sequences, groups (0: no shared segments), sequences a group
   int Hkv, R, S, RS;          // key heads, query heads a key head, queries, R * S
+  float inv_N, inv_S, inv_RS;
   int n_pages, lp, max_pages, causal;
   int TRp, TRo;               // rows of a row tile: shared segments, own segments
   int TR;                     // the larger of the two: rows of a partial row tile's place
-  Cost cp, co;                // units of a row tile: shared segments, own segments
+  int cp, co;                 // cost of a row tile: shared segments, own segments
   Log2Scale c;
   int* shared_out;            // [G] shared tokens that the call takes once
   int2* parts;                // [row tiles] first slot, parts (0: none, 1: the whole tile)
   int nrtp, nrto;             // row tiles of a segment
+  float inv_nrtp, inv_nrto;
   float* full;                // [2][B * Hq * S][D] partial rows of whole row tiles
   float2* full_ml;            // [2][B * Hq * S]
   float* piece;               // [2 slots][TR][D] partial rows of shared row tiles
@@ -88,13 +87,29 @@ __device__ __forceinline__ int seq_queries(const Args& a, int b) {
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-// x / y for 0 <= x < 2^31, y > 0 and a quotient below 2^20, inv = 1.f / y: the product is
-// off by less than one.
+// x / y for 0 <= x < 2^30, 0 < y, inv = 1.f / y.  The product is off by less than one for
+// quotients below 2^21; the kernel's start is bound by cold instruction fetches, and an
+// integer division is some thirty of them.
 __device__ __forceinline__ int div_small(int x, int y, float inv) {
   int q = static_cast<int>(static_cast<float>(x) * inv);
   q -= q * y > x;
-  q += (q + 1) * y <= x;
+  q += x - q * y >= y;
   return q;
+}
+
+__device__ __forceinline__ int group_of(const Args& a, int b) { return div_small(b, a.N, a.inv_N); }
+// Query of a row within (sequence, key head).
+__device__ __forceinline__ int query_of(const Args& a, int in) {
+  return in - div_small(in, a.S, a.inv_S) * a.S;
+}
+
+// An address that is the same in every lane, as the copies need it, for certain.
+template <typename P>
+__device__ __forceinline__ const P* uniform(const P* p) {
+  const uint64_t x = reinterpret_cast<uint64_t>(p);
+  const uint64_t lo = static_cast<uint32_t>(uniform(static_cast<int>(x)));
+  const uint64_t hi = static_cast<uint32_t>(uniform(static_cast<int>(x >> 32)));
+  return reinterpret_cast<const P*>(hi << 32 | lo);
 }
 
 // Prefix sums of the segments' units of one head, the sequences' lengths, and the shared
@@ -108,11 +123,8 @@ struct Schedule {
   int most;  // units of the longest row tile
 };
 
-__device__ __forceinline__ Cost cost_of(const Args& a, bool shared) {
-  return Cost{shared ? a.cp.row : a.co.row, shared ? a.cp.tile : a.co.tile};
-}
-__device__ __forceinline__ int row_units(const Cost& c, int keys) {
-  return c.row + c.tile * ceil_div(keys, kTile);
+__device__ __forceinline__ int row_units(int cost, int keys) {
+  return cost + ceil_div(keys, kTile);
 }
 
 template <int W>
@@ -127,7 +139,7 @@ __device__ void build_schedule(const Args& a, Schedule& s) {
     s.len[b] = len;
     if (a.G == 0) atomicMax(&s.most, row_units(a.co, len));
     if (a.G > 0 && len > 0)
-      atomicMin(&s.sh[b / a.N], a.causal ? max(min(len - seq_queries(a, b) + 1, len), 0) : len);
+      atomicMin(&s.sh[group_of(a, b)], a.causal ? max(min(len - seq_queries(a, b) + 1, len), 0) : len);
   }
   __syncthreads();
   if (a.G > 0) {
@@ -143,7 +155,7 @@ __device__ void build_schedule(const Args& a, Schedule& s) {
   auto units = [&](int i) {
     if (i < a.G) return s.sh[i] == 0 ? 0 : a.nrtp * row_units(a.cp, s.sh[i]);
     const int b = i - a.G;
-    return a.nrto * row_units(a.co, a.G > 0 ? max(s.len[b] - s.sh[b / a.N], 0) : s.len[b]);
+    return a.nrto * row_units(a.co, a.G > 0 ? max(s.len[b] - s.sh[group_of(a, b)], 0) : s.len[b]);
   };
   int sum = 0;
   for (int i = i0; i < i1; ++i) sum += units(i);
@@ -191,10 +203,10 @@ __device__ __forceinline__ Row row_of(const Args& a, const Job& j, int rho) {
   Row r;
   r.inside = rho < j.rows;
   rho = r.inside ? rho : j.rows - 1;
-  const int k = j.shared ? rho / a.RS : 0;
+  const int k = j.shared ? div_small(rho, a.RS, a.inv_RS) : 0;
   r.b = j.b0 + k;
   r.in = rho - k * a.RS;
-  r.real = r.inside && r.in % a.S < seq_queries(a, r.b);
+  r.real = r.inside && query_of(a, r.in) < seq_queries(a, r.b);
   return r;
 }
 __device__ __forceinline__ size_t row_index(const Args& a, int h, const Row& r) {
@@ -223,6 +235,8 @@ struct PageCursor {
   // Row of the pool (in tokens of one head, page 0 for an entry that is no page) that
   // holds position pos, pos being at most 64 pages behind the last one asked for.
   __device__ __forceinline__ size_t row(int pos, int h, int Hkv) {
+    pos = uniform(pos);
+    h = uniform(h);
     int i = __builtin_amdgcn_readfirstlane(pos >> lp) - base;
     if (i >= 64) {
       base += 64;
@@ -263,7 +277,7 @@ __device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xC07F);
 // Last key position that a row sees, plus one.
 __device__ __forceinline__ int row_end(const Args& a, const Job& j, const Row& r) {
   if (!a.causal || j.shared) return j.pos1;
-  const int last = seq_tokens(a, r.b) - seq_queries(a, r.b) + r.in % a.S;
+  const int last = seq_tokens(a, r.b) - seq_queries(a, r.b) + query_of(a, r.in);
   return min(j.pos1, last + 1);
 }
 
@@ -414,11 +428,11 @@ __device__ void attend_few(const Args& a, const Job& j, char* lds_all, float2* l
     if (once) {
 #pragma unroll
       for (int i = 0; i < NI; ++i)
-        lds_dma16_once(p + off[i & 1], voff + 64 * (i >> 1), to + (i >> 1) * 2048 + (i & 1) * 1024);
+        lds_dma16_once(uniform(p + off[i & 1]), voff + 64 * (i >> 1), to + (i >> 1) * 2048 + (i & 1) * 1024);
     } else {
 #pragma unroll
       for (int i = 0; i < NI; ++i)
-        lds_dma16(p + off[i & 1], voff + 64 * (i >> 1), to + (i >> 1) * 2048 + (i & 1) * 1024);
+        lds_dma16(uniform(p + off[i & 1]), voff + 64 * (i >> 1), to + (i >> 1) * 2048 + (i & 1) * 1024);
     }
   };
 
@@ -655,14 +669,14 @@ __device__ void attend_many(const Args& a, const Job& j, char* lds) {
     const size_t off0 = look(0);
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      lds_dma16(kp + off0 + 64 * i, voff, kdst(0) + i * 4096);
-      lds_dma16(vp + off0 + 64 * i, voff, vdst(0) + i * 4096);
+      lds_dma16(uniform(kp + off0) + 64 * i, voff, kdst(0) + i * 4096);
+      lds_dma16(uniform(vp + off0) + 64 * i, voff, vdst(0) + i * 4096);
     }
     off1 = off0;
     if (T > 1) {
       off1 = look(1);
 #pragma unroll
-      for (int i = 0; i < NI; ++i) lds_dma16(kp + off1 + 64 * i, voff, kdst(1) + i * 4096);
+      for (int i = 0; i < NI; ++i) lds_dma16(uniform(kp + off1) + 64 * i, voff, kdst(1) + i * 4096);
     }
     wait_dma();
     __syncthreads();
@@ -715,8 +729,8 @@ __device__ void attend_many(const Args& a, const Job& j, char* lds) {
     if (t + 1 >= T_full && t + 1 < T) mask(t + 1, sn0, sn1);
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      lds_dma16(kp + off2 + 64 * i, voff, kdst(t) + i * 4096);
-      lds_dma16(vp + off1 + 64 * i, voff, vdst(t + 1) + i * 4096);
+      lds_dma16(uniform(kp + off2) + 64 * i, voff, kdst(t) + i * 4096);
+      lds_dma16(uniform(vp + off1) + 64 * i, voff, vdst(t + 1) + i * 4096);
     }
     uint32_t pb[16];
 #pragma unroll
@@ -750,8 +764,8 @@ __device__ void attend_many(const Args& a, const Job& j, char* lds) {
   // and the copies are spread over the Q K^T phase.
   auto main_iter = [&](int t, f32x16& c0, f32x16& c1, f32x16& n0, f32x16& n1) {
     const size_t off2 = t + 2 < T ? look(t + 2) : off1;
-    const char* kbase = kp + off2;
-    const char* vbase = vp + off1;
+    const char* kbase = uniform(kp + off2);
+    const char* vbase = uniform(vp + off1);
     off1 = off2;
     rescale();
     const char* Kb = kbuf(t + 1);
@@ -933,7 +947,7 @@ __device__ void attend_f32(const Args& a, const Job& j, char* lds_all, float2* l
   };
   auto load = [&](int pos, int buf, Piece& x) {
     const size_t at = cur.row(pos, j.h, a.Hkv) * D;
-    kt.copy(static_cast<const float*>(a.kp) + at, 0, kF32Keys, buf);
+    kt.copy(uniform(static_cast<const float*>(a.kp) + at), 0, kF32Keys, buf);
     const float* v = static_cast<const float*>(a.vp) + at;
 #pragma unroll
     for (int s = 0; s < 4; ++s)
@@ -1037,11 +1051,31 @@ constexpr int attend_lds() {
 }
 
 // ---- the runs ---------------------------------------------------------------------------
-// Run c is units [c * run, (c + 1) * run), its ends moved to a row tile's end where they
-// would leave less than kSnap tiles on either side.
-__device__ __forceinline__ int run_units(int total, int slots) {
-  const int run = ceil_div(total, slots);
-  return run < kRunMin ? kRunMin : run;
+// Run c of n begins at unit c * total / n (at c * kRunMin in a small call), or at a row
+// tile's end where that would leave less than kSnap tiles on either side.
+struct Runs {
+  int total, n;  // n <= 512 runs
+  bool small;    // of kRunMin units each
+};
+__device__ __forceinline__ Runs runs_of(int total, int slots) {
+  const bool small = total < slots * kRunMin;
+  return {total, small ? ceil_div(total, kRunMin) : slots, small};
+}
+__device__ __forceinline__ int run_begin(const Runs& r, int c) {
+  return r.small ? min(c * kRunMin, r.total)
+                 : static_cast<int>(static_cast<long long>(r.total) * c / r.n);
+}
+// The last run that begins at unit x or before.
+__device__ __forceinline__ int run_at(const Runs& r, int x) {
+  int c = static_cast<int>(static_cast<float>(x) *
+                           (r.small ? 1.f / kRunMin : r.n / static_cast<float>(r.total)));
+  while (c > 0 && run_begin(r, c) > x) --c;
+  while (c + 1 < r.n && run_begin(r, c + 1) <= x) ++c;
+  return c;
+}
+// Whether a row tile may be cut at its unit k.
+__device__ __forceinline__ bool cuts(int cost, int per, int k) {
+  return k >= cost + kSnap && k <= per - kSnap;
 }
 
 // Where unit u lies: its head, segment, row tile, the units of the row tile before it, and
@@ -1058,18 +1092,15 @@ __device__ __forceinline__ Place place_of(const Args& a, const Schedule& s, int 
   int before = 0;  // segments that start at or before `in`: the last of them is not empty
   for (int i = 0; i < n; i += 64) before += __popcll(__ballot(i + lane < n && s.off[i + lane] <= in));
   p.seg = uniform(before) - 1;
-  const int b = p.seg - a.G;
-  const int keys = p.seg < a.G ? s.sh[p.seg]
-                               : a.G > 0 ? max(s.len[b] - s.sh[b / a.N], 0) : s.len[b];
-  p.per = uniform(row_units(cost_of(a, p.seg < a.G), keys));
-  const int x = in - s.off[p.seg];
-  p.rt = uniform(x / p.per);
-  p.k = uniform(x) - p.rt * p.per;
+  const bool shared = p.seg < a.G;
+  const int units = uniform(s.off[p.seg + 1]) - uniform(s.off[p.seg]);
+  const int tiles = shared ? a.nrtp : a.nrto;
+  p.per = units;
+  if (tiles > 1) p.per = uniform(div_small(units, tiles, shared ? a.inv_nrtp : a.inv_nrto));
+  const int x = in - uniform(s.off[p.seg]);
+  p.rt = uniform(div_small(x, p.per, 1.f / static_cast<float>(p.per)));
+  p.k = x - p.rt * p.per;
   return p;
-}
-// Whether a row tile may be cut at its unit k.
-__device__ __forceinline__ bool cuts(const Cost& c, int per, int k) {
-  return k >= c.row + kSnap * c.tile && k <= per - kSnap * c.tile;
 }
 
 // How the row tiles reach the workgroups: kRuns as above; kWhole one row tile a workgroup,
@@ -1143,52 +1174,55 @@ prefix_attention_kernel(const Args a, Split split) {
     total = uniform(__shfl(upto, 63, 64));
     t += in_xcd;
   }
-  // The run: units [u, stop) of the call or, after the rounds, of the XCD's rest.
+  // The run: units [u, stop) of the call or, after the rounds, of the XCD's rest.  The first
+  // two turns of the loop move its ends to where row tiles may be cut.
   const int my = rounds ? in_xcd : slot;
-  const int run = whole ? 1 : run_units(total, rounds ? slots_xcd : gridDim.x);
-  auto place = [&](int x) {
-    if (!rounds) return place_of(a, s, per_head, inv_head, x);
-    Place p;
-    const int i = uniform(__popcll(__ballot(upto <= x)));
-    p.per = __builtin_amdgcn_readlane(per_l, i);
-    p.k = x - (__builtin_amdgcn_readlane(upto, i) - p.per);
-    const Tile y = tile_of(a, rest + i);
-    p.h = y.h;
-    p.seg = y.b;
-    p.rt = y.rt;
-    return p;
-  };
-  // an end inside a row tile where it is not cut moves to the tile's beginning or end
-  auto settle = [&](int x) {
-    const Place p = place(x);
-    const Cost c = cost_of(a, p.seg < a.G);
-    if (cuts(c, p.per, p.k)) return x;
-    return p.k < c.row + kSnap * c.tile ? x - p.k : x - p.k + p.per;
-  };
-  int u = 0, stop = 0;
-  if (!whole && my < ceil_div(total, run)) {
-    u = my > 0 ? settle(my * run) : 0;
-    stop = total - my * run > run ? settle(my * run + run) : total;
+  const Runs runs = runs_of(total, rounds ? slots_xcd : gridDim.x);
+  int u = 0, stop = 0, turn = 2;
+  if (!whole && my < runs.n && total > 0) {
+    u = uniform(run_begin(runs, my));
+    stop = my + 1 < runs.n ? uniform(run_begin(runs, my + 1)) : total;
+    turn = 0;
   }
-  for (;;) {
+  for (;; ++turn) {
     Place p;
-    int take, last = 0;  // slots behind this one that hold parts of a row tile begun here
-    if ((whole && t < end) || (rounds && t < rest)) {
+    int take = 0, last = 0;  // slots behind this one that hold parts of a row tile begun here
+    if (turn >= 2 && t < (rounds ? rest : whole ? end : 0)) {
       const Tile x = tile_of(a, t);
       p = Place{x.h, a.G + x.b, x.rt, 0, row_units(a.co, whole ? 0 : s.len[x.b])};
       take = p.per;
       t = whole ? end : t + slots_xcd;
-    } else if (u < stop) {
-      p = place(u);
+    } else {
+      const int x = turn == 1 ? stop : u;
+      if (turn >= 2 && u >= stop) break;
+      if (turn == 1 && stop == total) continue;
+      if (rounds) {
+        const int i = uniform(__popcll(__ballot(upto <= x)));
+        p.per = __builtin_amdgcn_readlane(per_l, i);
+        p.k = x - (__builtin_amdgcn_readlane(upto, i) - p.per);
+        const Tile y = tile_of(a, rest + i);
+        p.h = y.h;
+        p.seg = y.b;
+        p.rt = y.rt;
+      } else {
+        p = place_of(a, s, per_head, inv_head, x);
+      }
+      const int cost = p.seg < a.G ? a.cp : a.co;
+      if (turn < 2) {
+        int y = x;
+        if (!cuts(cost, p.per, p.k)) y = p.k < cost + kSnap ? x - p.k : x - p.k + p.per;
+        if (turn == 0)
+          u = uniform(y);
+        else
+          stop = uniform(y);
+        continue;
+      }
       take = min(stop - u, p.per - p.k);
       // those whose runs begin inside the row tile
-      if (take < p.per)
-        last = (u - p.k + p.per - kSnap * cost_of(a, p.seg < a.G).tile) / run - my;
+      if (take < p.per && p.k == 0) last = run_at(runs, u + p.per - kSnap) - my;
       u += take;
-    } else {
-      break;
     }
-    const Cost c = cost_of(a, p.seg < a.G);
+    const int cost = p.seg < a.G ? a.cp : a.co;
     Job j;
     int tile;  // the row tile's number in `parts`
     j.h = p.h;
@@ -1208,13 +1242,13 @@ prefix_attention_kernel(const Args a, Split split) {
       const int len = whole ? seq_tokens(a, j.b0) : s.len[j.b0];
       j.rows = a.RS;
       j.row0 = p.rt * a.TRo;
-      j.pos0 = uniform(a.G > 0 ? min(s.sh[j.b0 / a.N], len) : 0);
+      j.pos0 = uniform(a.G > 0 ? min(s.sh[group_of(a, j.b0)], len) : 0);
       j.pos1 = uniform(len);
       j.pages = a.table + static_cast<size_t>(j.b0) * a.max_pages;
       tile = a.G * a.Hkv * a.nrtp + (j.b0 * a.Hkv + p.h) * a.nrto + p.rt;
     }
-    j.t0 = uniform(max(p.k - c.row, 0) / c.tile);
-    j.t1 = uniform(whole ? ceil_div(j.pos1, kTile) : max(p.k + take - c.row, 0) / c.tile);
+    j.t0 = uniform(max(p.k - cost, 0));
+    j.t1 = uniform(whole ? ceil_div(j.pos1, kTile) : max(p.k + take - cost, 0));
     j.whole = take == p.per;
     j.piece = 2 * slot + (p.k > 0 ? 0 : 1);
     if (!whole && p.k == 0 && threadIdx.x == 0)
@@ -1255,12 +1289,12 @@ prefix_combine_kernel(const Args a, int chunk) {
   // one row tile, and written already unless it is cut
   if (a.G == 0 && chunk <= a.TRo && own[first_row / a.TRo].y <= 1) return;
   const int nq = seq_queries(a, b), len = a.seq_len[b];
-  const int g = a.G > 0 ? b / a.N : 0;
+  const int g = a.G > 0 ? group_of(a, b) : 0;
   const bool shared = a.G > 0 && len > 0 && a.shared_out[g] > 0;
   const size_t rows = static_cast<size_t>(a.B) * a.Hkv * a.RS;
   for (int r0 = first_row; r0 < last_row; r0 += RA) {
     const int in = min(r0 + ra, a.RS - 1);
-    const bool real = r0 + ra < last_row && in % a.S < nq;
+    const bool real = r0 + ra < last_row && query_of(a, in) < nq;
     const size_t row = static_cast<size_t>(pair) * a.RS + in;
     const int2 po = own[in / a.TRo];
     const int rho = (b - g * a.N) * a.RS + in;  // among the group's rows
@@ -1395,6 +1429,9 @@ void launch_prefix_attention(const PrefixCall& p, int dtype, int d, char* ws, hi
   a.R = p.Hq / p.Hkv;
   a.S = p.S;
   a.RS = a.R * p.S;
+  a.inv_N = a.N > 0 ? 1.f / static_cast<float>(a.N) : 0.f;
+  a.inv_S = 1.f / static_cast<float>(a.S);
+  a.inv_RS = 1.f / static_cast<float>(a.RS);
   a.n_pages = p.n_pages;
   a.lp = __builtin_ctz(static_cast<unsigned>(p.page));
   a.max_pages = p.max_pages;
@@ -1402,7 +1439,7 @@ void launch_prefix_attention(const PrefixCall& p, int dtype, int d, char* ws, hi
   a.TRp = w.shared_rows;
   a.TRo = w.own_rows;
   a.TR = w.piece_rows;
-  const auto cost = [&](int rows) { return rows == kManyRows ? Cost{4, 1} : Cost{6, 1}; };
+  const auto cost = [&](int rows) { return rows == kManyRows ? 4 : 6; };
   a.cp = cost(a.TRp);
   a.co = cost(a.TRo);
   a.c = log2_scale(p.scale);
@@ -1410,6 +1447,8 @@ void launch_prefix_attention(const PrefixCall& p, int dtype, int d, char* ws, hi
   a.parts = reinterpret_cast<int2*>(ws + w.parts);
   a.nrtp = w.groups > 0 ? ceil_div(a.N * a.RS, a.TRp) : 0;
   a.nrto = ceil_div(a.RS, a.TRo);
+  a.inv_nrtp = a.nrtp > 0 ? 1.f / static_cast<float>(a.nrtp) : 0.f;
+  a.inv_nrto = 1.f / static_cast<float>(a.nrto);
   a.full = reinterpret_cast<float*>(ws + w.full);
   a.full_ml = reinterpret_cast<float2*>(ws + w.full_ml);
   a.piece = reinterpret_cast<float*>(ws + w.piece);

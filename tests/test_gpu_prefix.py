@@ -57,7 +57,18 @@ def f64(x):
 
 
 def check(q, kp, vp, table, lens, scale, shared=None, q_len=None, causal=False, want=None):
-    """Runs the call on poisoned outputs and compares it; returns (o, lse)."""
+    """Runs the call on poisoned outputs and compares it, with the table as given and with
+    rows that have room for 5000 tokens more (the length of the rows decides how the work is
+    cut up); returns (o, lse) of the first."""
+    if want is None:
+        want = pages.paged_attention(f64(q), f64(kp), f64(vp), table, lens, scale, q_len, causal)
+    wide = [list(r) + [-1] * (5000 // kp.shape[2]) for r in table]
+    check_one(q, kp, vp, wide, [min(n, len(table[0]) * kp.shape[2]) for n in lens], scale, shared,
+              q_len, causal, want)
+    return check_one(q, kp, vp, table, lens, scale, shared, q_len, causal, want)
+
+
+def check_one(q, kp, vp, table, lens, scale, shared, q_len, causal, want):
     B, Hq, S, d = q.shape
     bf = q.dtype == torch.bfloat16
     o = torch.full_like(q, 7.0)
@@ -67,8 +78,6 @@ def check(q, kp, vp, table, lens, scale, shared=None, q_len=None, causal=False, 
         shared_len=None if shared is None else torch.tensor(shared, **I32),
         q_len=None if q_len is None else torch.tensor(q_len, **I32), causal=causal, o=o, lse=lse)
     torch.cuda.synchronize()
-    if want is None:
-        want = pages.paged_attention(f64(q), f64(kp), f64(vp), table, lens, scale, q_len, causal)
     ro, rl, size = want
     got_o, got_l = f64(o), f64(lse)
     real = ~np.isnan(rl)
