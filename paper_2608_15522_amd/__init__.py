@@ -28,3 +28,4 @@ from .binding import (  # noqa: F401
     SA_ERR_INVALID_ARG, SA_ERR_UNSUPPORTED, SA_ERR_WORKSPACE, SA_ERR_HIP,
 )
 from .layer import protected_sparse_layer  # noqa: F401
+from .pages import KVPages  # noqa: F401

@@ -306,3 +306,55 @@ def test_captured_calls_follow_the_lists():
     for a, b in zip(*results):
         assert all(torch.equal(p, q) for p, q in zip(a, b))
     assert results[0][-1][3].tolist()[0] > 0
+
+
+def test_pages_of_several_layers_through_the_class():
+    """KVPages: two layers, samples forked from one prompt, grown, dropped and compacted;
+    each layer's attention is that over what was written for it."""
+    B, Hkv, Hq, d, S, layers = 4, 2, 4, 64, 40, 2
+    cache = sa.KVPages(B, 400, 40, Hkv, d, page=32, layers=layers, dtype=torch.float32)
+    g = torch.Generator(device="cuda").manual_seed(6)
+    have = [[[torch.empty(Hkv, 0, d, device="cuda")] * 2 for _ in range(B)] for _ in range(layers)]
+
+    def grow(new):
+        m = ints(new)
+        assert cache.reserve(m).item() == 0
+        for layer in range(layers):
+            k, v = (torch.randn(B, Hkv, S, d, device="cuda", generator=g) for _ in range(2))
+            cache.write(layer, k, v, m)
+            for b, c in enumerate(new):
+                have[layer][b] = [torch.cat([x, y[b, :, :c]], 1)
+                                  for x, y in zip(have[layer][b], (k, v))]
+
+    def look(shared):
+        for layer in range(layers):
+            q = torch.randn(B, Hq, 3, d, device="cuda", generator=g)
+            o, lse = cache.attend(layer, q, 0.125, want_lse=True, shared_len=ints([shared]))
+            for b in range(B):
+                k, v = (x.double().repeat_interleave(Hq // Hkv, 0) for x in have[layer][b])
+                x = torch.matmul(q[b].double(), k.transpose(1, 2).contiguous()) * 0.125
+                if k.shape[1] == 0:
+                    assert (o[b] == 0).all() and (lse[b] == -float("inf")).all()
+                    continue
+                # scores below 16 in magnitude: weights and lse to 2^-24 * (d + 4) * 16, |v| < 6
+                assert (lse[b].double() - x.logsumexp(-1)).abs().max() <= 7e-5
+                assert (o[b].double() - torch.matmul(x.softmax(-1), v)).abs().max() <= 9e-4
+
+    grow([37, 0, 0, 0])
+    grow([40, 0, 0, 0])
+    look(0)
+    assert cache.fork(ints([0, 0, 0]), ints([1, 2, 3])).item() == 0
+    for layer in range(layers):
+        for b in range(1, B):
+            have[layer][b] = list(have[layer][0])
+    grow([1, 40, 7, 32])
+    look(64)
+    cache.free(ints([0, 2]))
+    for layer in range(layers):
+        for b in (0, 2):
+            have[layer][b] = [x[:, :0] for x in have[layer][b]]
+    counts = cache.compact()
+    assert counts[0].item() == (cache.page_ref > 0).sum().item()
+    look(64)
+    grow([5, 3, 0, 40])
+    look(64)
