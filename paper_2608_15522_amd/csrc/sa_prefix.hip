@@ -248,18 +248,17 @@ struct PageCursor {
     p = p >= 0 && p < n_pages ? p : 0;
     return (((static_cast<size_t>(p) * Hkv + h) << lp) + (pos & ((1 << lp) - 1)));
   }
+  // Whether an entry between the cursor's start and position `end` is no page: its keys are
+  // left out.  The entries that start() loads, and what lies behind them.
+  __device__ __forceinline__ bool bad(int end) const {
+    const int last = ceil_div(end, 1 << lp), lane = threadIdx.x & 63;
+    auto none = [&](int i, int p) { return i < last && (p < 0 || p >= n_pages); };
+    bool b = none(base + lane, cur) || none(base + 64 + lane, next);
+    for (int i = base + 128; i < last; i += 64) b = b || none(i + lane, load(i));
+    return __any(b);
+  }
 };
 
-// Whether a table entry of positions [pos, end) is no page: its keys are left out.
-__device__ __forceinline__ bool bad_pages(const Args& a, const int32_t* pages, int pos, int end) {
-  bool bad = false;
-  const int last = ceil_div(end, 1 << a.lp);
-  for (int i = (pos >> a.lp) + (threadIdx.x & 63); i < last; i += 64) {
-    const int p = pages[i];
-    bad = bad || p < 0 || p >= a.n_pages;
-  }
-  return __any(bad);
-}
 __device__ __forceinline__ bool bad_page(const Args& a, const int32_t* pages, int pos) {
   const int i = pos >> a.lp;
   if (i >= a.max_pages) return true;
@@ -398,7 +397,7 @@ __device__ void attend_few(const Args& a, const Job& j, char* lds_all, float2* l
   for (int kc = 0; kc < KC; ++kc)
     qf[kc] = row.inside ? ldg16(q + row_index(a, j.h, row) * D + 16 * kc + 8 * g)
                         : u32x4{0u, 0u, 0u, 0u};
-  const bool bad = bad_pages(a, j.pages, run0, run1);
+  const bool bad = cur.bad(run1);
   const int end = row_end(a, j, row);
 
   // DMA: 1 KB = 16 rows of one 32-channel plane; lane l's source is the 16-byte slot that
@@ -589,7 +588,9 @@ __device__ void attend_many(const Args& a, const Job& j, char* lds) {
     most = min(run1, q0 + min(one ? last % a.S : a.S - 1, nq - 1));
     least = min(run1, q0 + (one ? j.row0 % a.S : 0));
   }
-  const bool bad = bad_pages(a, j.pages, run0, run1);
+  PageCursor cur;  // from the same page in every wave, so that all find the same
+  cur.start(a, j.pages, run0);
+  const bool bad = cur.bad(run1);
   const int T = most > run0 ? ceil_div(most - run0, kTile) : 0;
   // leading tiles that every row sees whole
   const int T_full = bad || least <= run0 ? 0 : min((least - run0) / kTile, T);
@@ -615,8 +616,6 @@ __device__ void attend_many(const Args& a, const Job& j, char* lds) {
   auto vbuf = [&](int t) -> char* { return lds + (2 + (t & 1)) * TILE; };
   const char* kp = static_cast<const char*>(a.kp);
   const char* vp = static_cast<const char*>(a.vp);
-  PageCursor cur;
-  cur.start(a, j.pages, run0 + 16 * wave);
   // byte offset of the wave's group of tile t, the same in K and V
   auto look = [&](int t) { return cur.row(run0 + kTile * t + 16 * wave, j.h, a.Hkv) * (D * 2); };
 
@@ -938,7 +937,7 @@ __device__ void attend_f32(const Args& a, const Job& j, char* lds_all, float2* l
   for (int i = 0; i < KI; ++i)
     qf[i] = row.inside ? ldg_f32x4(q + row_index(a, j.h, row) * D + 16 * i + 4 * gk)
                        : f32x4{0.f, 0.f, 0.f, 0.f};
-  const bool bad = bad_pages(a, j.pages, run0, run1);
+  const bool bad = cur.bad(run1);
   const int end = row_end(a, j, row);
   KTile kt;
   kt.init(lds, lane);
