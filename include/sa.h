@@ -437,7 +437,7 @@ int sa_cache_indicator(const void* y_v, const void* y_v_hat,
  *   seq_len           [B] i32: tokens of each sequence (negative counts as 0)
  *   page_ref          [n_pages] i32: how many table entries name the page; 0 = free
  * page in {16, 32, 64, 128}; max_pages * page <= 2^30; B <= 16384 (the attention:
- * B + n_groups <= 1024).  Every list lives on the device, so the calls can be
+ * B + n_groups <= 1024, B * Hkv <= 65535).  Every list lives on the device, so the calls can be
  * captured into a HIP graph and follow the lists' values at each replay.  Calls
  * on one cache that may overlap in time must be ordered by the caller.
  */
@@ -482,7 +482,7 @@ int sa_pages_write(const void* k, const void* v, void* k_pages, void* v_pages,
  * fresh page, so that both sequences can go on writing: the pair (copy_src[i],
  * copy_dst[i]) is to be copied in every pool with sa_pages_copy before either is
  * written; both are -1 where there is nothing to copy.  An entry whose src has
- * no tokens, whose dst has some, or that names a sequence outside [0,B) is left
+ * no tokens (or more than its table row), whose dst has some, or that names a sequence outside [0,B) is left
  * out, and of several entries with one dst the first counts.  Fresh pages are
  * the lowest free ones, in the order of the entries; with too few nothing is
  * changed, missing[0] is how many lack (otherwise 0), and all pairs are -1.
@@ -564,7 +564,10 @@ int sa_pages_copy(void* pools, int n_pools, int n_pages, size_t page_bytes,
  *   shared_len [n_groups] i32, NULL iff n_groups = 0
  *   q_len      [B] i32 (clamped to [0,S]), NULL = S for every sequence
  *   Hq         a multiple of Hkv
- *   ws         workspace of at least sa_prefix_attention_workspace(...) bytes
+ *   ws         workspace of at least sa_prefix_attention_workspace(...) bytes, of any
+ *              content; calls that may overlap in time need one each
+ * A call whose row tiles times the keys that max_pages has room for pass some 2^35
+ * (row tiles of 32 or 128 rows) is too large and returns SA_ERR_UNSUPPORTED.
  */
 int sa_prefix_attention(const void* q, const void* k_pages,
                         const void* v_pages, void* o, float* lse,

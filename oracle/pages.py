@@ -39,7 +39,8 @@ def fork(table, lens, ref, src, dst, page):
     B, n = len(lens), len(src)
     pairs, seen = [], set()
     for i, (a, b) in enumerate(zip(map(int, src), map(int, dst))):
-        if not (0 <= a < B and 0 <= b < B) or lens[a] <= 0 or lens[b] > 0 or b in seen:
+        if not (0 <= a < B and 0 <= b < B) or b in seen or not (
+                0 < lens[a] <= len(table[0]) * page and lens[b] <= 0):
             continue
         seen.add(b)
         pairs.append((i, a, b))

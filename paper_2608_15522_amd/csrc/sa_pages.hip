@@ -198,11 +198,12 @@ pages_reserve_kernel(int32_t* __restrict__ table, int32_t* __restrict__ seq_len,
   });
 }
 
-// Entries of a fork: src must hold tokens and dst none, so the two sets are disjoint;
-// of several entries with one dst the first able one counts.
+// Entries of a fork: src must hold tokens (no more than its row has room for) and dst none,
+// so the two sets are disjoint; of several entries with one dst the first able one counts.
 __device__ __forceinline__ bool fork_able(const int32_t* __restrict__ seq_len, int src, int dst,
-                                          int B) {
-  return src >= 0 && src < B && dst >= 0 && dst < B && seq_len[src] > 0 && seq_len[dst] <= 0;
+                                          int B, int capacity) {
+  return src >= 0 && src < B && dst >= 0 && dst < B && seq_len[src] > 0 &&
+         seq_len[src] <= capacity && seq_len[dst] <= 0;
 }
 
 // dst's row is src's, with the fresh page in the place of the partial last one, and every
@@ -241,7 +242,7 @@ pages_fork_plan_kernel(int32_t* __restrict__ table, int32_t* __restrict__ seq_le
   const int i0 = min(tid * each, n), i1 = min(i0 + each, n);
   unsigned counts = 0, part = 0;  // of the thread's entries: those that count, with a partial page
   for (int i = i0; i < i1; ++i)
-    if (fork_able(seq_len, src[i], dst[i], B)) {
+    if (fork_able(seq_len, src[i], dst[i], B, max_pages << lp)) {
       counts |= 1u << (i - i0);
       atomicMin(&first[dst[i]], i);
     }
@@ -265,8 +266,7 @@ pages_fork_plan_kernel(int32_t* __restrict__ table, int32_t* __restrict__ seq_le
     if (lacking == 0 && ((counts >> (i - i0)) & 1)) {
       const int full = seq_len[src[i]] >> lp;
       const bool partial = (part >> (i - i0)) & 1;
-      last = partial && full < max_pages ? table[static_cast<size_t>(src[i]) * max_pages + full]
-                                         : -1;
+      last = partial ? table[static_cast<size_t>(src[i]) * max_pages + full] : -1;
       last = max(last, -1);  // an entry that is no page: nothing to copy
       if (partial) entry[rank++] = i;
     }

@@ -54,7 +54,8 @@ bool prefix_sizes_ok(int B, int Hq, int Hkv, int S, int d, int dtype, int n_grou
   return B >= 1 && Hkv >= 1 && Hq >= Hkv && Hq % Hkv == 0 && S >= 1 && S <= sa::kMaxTokens &&
          (d == 64 || d == 128) && (dtype == SA_BF16 || dtype == SA_F32) && n_groups >= 0 &&
          n_groups <= B && (n_groups == 0 || B % n_groups == 0) &&
-         static_cast<long long>(B) + n_groups <= sa::kMaxAttendSegs && Hkv <= 65535 &&
+         static_cast<long long>(B) + n_groups <= sa::kMaxAttendSegs &&
+         static_cast<long long>(B) * Hkv <= sa::kMaxPairs &&
          static_cast<long long>(B) * Hq <= kMaxRows / S;
 }
 
@@ -203,7 +204,9 @@ int sa_prefix_attention(const void* q, const void* k_pages, const void* v_pages,
                 sa::kMaxAttendSegs);
   if (static_cast<long long>(B) * Hq > kMaxRows / S)
     return fail(SA_ERR_UNSUPPORTED, "%s: B=%d Hq=%d S=%d is too large", fn, B, Hq, S);
-  if (Hkv > 65535) return fail(SA_ERR_UNSUPPORTED, "%s: Hkv=%d exceeds 65535", fn, Hkv);
+  if (static_cast<long long>(B) * Hkv > sa::kMaxPairs)
+    return fail(SA_ERR_UNSUPPORTED, "%s: B*Hkv=%lld exceeds %d", fn,
+                static_cast<long long>(B) * Hkv, sa::kMaxPairs);
   if (sa::prefix_units(B, Hq, Hkv, S, d, dtype, n_groups,
                        static_cast<long long>(max_pages) * page) > 0x3fffffff)
     return fail(SA_ERR_UNSUPPORTED,

@@ -1386,11 +1386,15 @@ Plan plan_of(const Args& a, const PrefixCall& p, bool bf16, int d) {
                  : keys * d <= 1 << 17 && tiles * keys * d <= 1 << 25;
   } else if (many_own) {
     // 48 row tiles of 144 rows at d 128: 16 against 21 us with room for 1000 keys, 27 against
-    // 24 with room for 2000.  Under a causal mask the row tiles of a sequence whose queries
-    // are a quarter of its tokens or more see unequally many keys, which runs do not know: as
-    // many row tiles as slots suffice (528 of up to 1700 keys: 51 against 62 us).
-    whole = keys <= 1024 ||
-            (tiles >= kPrefixSlots && (keys <= 2048 || (p.causal && keys <= 4ll * p.S)));
+    // 24 with room for 2000.  Under a causal mask, where the queries are a quarter of a
+    // sequence's tokens or more, its row tiles see unequally many keys: 32 heads over 8, 1500
+    // queries, 81 against 101 us (96 row tiles: 39 against 48), 4000 queries of 8 heads (256
+    // row tiles of d 64) 65 against 58, of 32 heads 200 against 199.  Runs by the keys that
+    // each row tile sees took 67 and 64 us in the first and third of these, and up to twice
+    // as long as whole row tiles with fewer queries: they leave a head's keys to be read by
+    // workgroups at different places.
+    whole = keys <= 1024 || (tiles >= kPrefixSlots && keys <= 2048) ||
+            (p.causal && keys <= 4ll * p.S && (tiles >= kPrefixSlots || keys <= 4096));
   } else if (tiles <= kPrefixSlots / 2) {
     whole = bf16 ? keys <= 2048 : keys * d <= 1 << 16;
   } else {

@@ -92,6 +92,14 @@ def test_fork(B, n_pages, width, page, longest):
         same((t, n, r, a, b, missing), pages.fork(table, lens, ref, src, dst, page))
 
 
+def test_fork_of_a_length_beyond_the_row_is_left_out():
+    lists = ([[0, 1], [2, 3], [-1, -1], [-1, -1]], [33, 32, 0, -4], [1, 1, 1, 1, 0, 0])
+    t, n, r = on_gpu(lists)
+    a, b, missing = sa.sa_pages_fork(t, n, r, ints([0, 1]), ints([2, 3]), 16)
+    same((t, n, r, a, b, missing), pages.fork(*lists, [0, 1], [2, 3], 16))
+    assert n.tolist() == [33, 32, 0, 32]
+
+
 def test_fork_without_room_changes_nothing():
     lists = ([[0, 1], [2, -1], [-1, -1], [-1, -1]], [20, 16, 0, 0], [1, 1, 1])
     for src, dst in (([0, 1], [2, 3]), ([1, 1], [2, 3])):  # the second needs no fresh page

@@ -96,6 +96,8 @@ INVALID += [
     (_attend, dict(B=1025), UNS, "B=1025"),
     (_attend, dict(B=1000, n_groups=100), UNS, "B + n_groups = 1100"),
     (_attend, dict(B=1000, Hq=1 << 16, S=1 << 10), UNS, "too large"),
+    (_attend, dict(B=64, Hq=1024, Hkv=1024), UNS, "B*Hkv=65536"),
+    (_attend, dict(B=512, Hq=64, Hkv=64, S=64, max_pages=1 << 26), UNS, "too large for one call"),
     (_attend, dict(causal=2), ARG, "causal=2"), (_attend, dict(scale=0.0), ARG, "scale"),
     (_attend, dict(scale=float("nan")), ARG, "scale"), (_attend, dict(scale=-1.0), ARG, "scale"),
     (_attend, dict(q=None), ARG, "q is NULL"), (_attend, dict(o=FARTHEST + 8), ARG, "o is not 16"),
