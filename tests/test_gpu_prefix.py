@@ -92,8 +92,8 @@ def check_one(q, kp, vp, table, lens, scale, shared, q_len, causal, want):
     e = ((d + 4) * X + max(lens) + 64) * 2.0 ** -24
     assert np.isfinite(got_o[some]).all()
     # lse: the same relative error, and its own rounding
-    off = np.abs(got_l - rl)[some] - (e + 2.0 ** -22 * np.abs(rl))[some]
-    assert off.max(initial=-1) <= 0, f"lse off by {np.abs(got_l - rl)[some].max()}"
+    off = np.abs(got_l[some] - rl[some]) - (e[some] + 2.0 ** -22 * np.abs(rl[some]))
+    assert off.max(initial=-1) <= 0, f"lse off by {np.abs(got_l[some] - rl[some]).max()}"
     tol = 2 * e[..., None] * size + (2.0 ** -8 * (size * 1.02 + np.abs(ro)) if bf else
                                      2.0 ** -23 * np.abs(ro)) + 1e-37
     off = (np.abs(got_o - ro) - tol)[some]
@@ -248,6 +248,11 @@ def test_scores_of_every_size(dtype):
     ("f32", 16, 4, 1, 3, 64, 1024, 3, 400, 32),
     ("f32", 2, 2, 2, 100, 128, 512, 100, 700, 64),
     ("bf16", 512, 1, 1, 1, 64, 256, 0, 200, 16),       # as many segments as there may be
+    # more row tiles than slots of nearly the same length: whole ones first, the rest cut
+    ("bf16", 1, 16, 16, 4224, 64, 0, 4224, 4300, 128),
+    ("bf16", 130, 4, 4, 1, 128, 0, 2480, 2500, 64),
+    ("f32", 70, 8, 8, 2, 64, 0, 1500, 1510, 64),
+    ("bf16", 512, 8, 8, 1, 64, 0, 1, 60, 16),          # eight row tiles a slot
 ])
 @pytest.mark.parametrize("causal", [False, True])
 def test_larger_calls(dtype, B, Hq, Hkv, S, d, shared, lo, hi, page, causal):
@@ -256,30 +261,33 @@ def test_larger_calls(dtype, B, Hq, Hkv, S, d, shared, lo, hi, page, causal):
     lens[-1] = shared + hi
     q, kp, vp, table = make(B + S, lens, Hq, Hkv, S, d, page, dtype, [shared])
     want = reference(q, kp, vp, table, lens, d ** -0.5, causal)
-    for claim in ([shared], None) if B < 512 else ([shared] * 512, [shared]):
+    for claim in ([shared], None) if B < 512 or Hkv > 1 else ([shared] * 512, [shared]):
         o, lse = check(q, kp, vp, table, lens, d ** -0.5, shared=claim, causal=causal, want=want)
         again = check(q, kp, vp, table, lens, d ** -0.5, shared=claim, causal=causal, want=want)
         assert torch.equal(o, again[0]) and torch.equal(lse, again[1]), "run to run"
 
 
-def reference(q, kp, vp, table, lens, scale, causal):
+def reference(q, kp, vp, table, lens, scale, causal, q_len=None):
     """pages.paged_attention on the GPU, a sequence at a time (fp64)."""
     B, Hq, S, d = q.shape
     Hkv, page = kp.shape[1:3]
-    out = [torch.empty(B, Hq, S, d, dtype=torch.float64), torch.empty(B, Hq, S, dtype=torch.float64),
-           torch.empty(B, Hq, S, d, dtype=torch.float64)]
+    out = [torch.full((B, Hq, S, d), float("nan"), dtype=torch.float64),
+           torch.full((B, Hq, S), float("nan"), dtype=torch.float64),
+           torch.full((B, Hq, S, d), float("nan"), dtype=torch.float64)]
     for b, n in enumerate(lens):
-        ids = torch.tensor(table[b][:-(-n // page)], device="cuda")
+        new = S if q_len is None else q_len[b]
+        ids = torch.tensor(table[b][:-(-n // page)], dtype=torch.long, device="cuda")
         k, v = (p[ids].transpose(0, 1).reshape(Hkv, -1, d)[:, :n].double().repeat_interleave(
             Hq // Hkv, 0).contiguous() for p in (kp, vp))
-        x = torch.matmul(q[b].double(), k.transpose(1, 2).contiguous()) * scale
+        x = torch.matmul(q[b, :, :new].double(), k.transpose(1, 2).contiguous()) * scale
         if causal:
             see = (torch.arange(n, device="cuda") <=
-                   n - S + torch.arange(S, device="cuda")[:, None])
+                   n - new + torch.arange(new, device="cuda")[:, None])
             x = x.masked_fill(~see, -float("inf"))
-        w = x.softmax(-1)
-        out[0][b], out[1][b] = torch.matmul(w, v), x.logsumexp(-1)
-        out[2][b] = torch.matmul(w, v.abs())
+        z = x.logsumexp(-1)
+        w = torch.where(z[..., None] == -float("inf"), torch.zeros_like(x), (x - z[..., None]).exp())
+        out[0][b, :, :new], out[1][b, :, :new] = torch.matmul(w, v), z
+        out[2][b, :, :new] = torch.matmul(w, v.abs())
     return [t.cpu().numpy() for t in out]
 
 
@@ -414,3 +422,33 @@ def test_a_generation_chunk_by_chunk():
     for new in ([1, 1, 0, 1, 1], [24, 2, 20, 24, 1]):
         grow(new)
         look(new, shared, True)
+
+
+@pytest.mark.parametrize("seed", range(48))
+def test_random_calls(seed):
+    """Sizes, types, groups, masks, lengths and table widths drawn together, so that every
+    way of cutting a call up is met."""
+    rng = random.Random(1000 + seed)
+    dtype = "f32" if seed % 4 == 3 else "bf16"
+    page, d = rng.choice([16, 32, 64, 128]), rng.choice([64, 128])
+    Hkv, R = rng.choice([1, 2, 3, 8]), rng.choice([1, 1, 2, 5, 8])
+    groups, per = rng.choice([1, 1, 2, 3]), rng.choice([1, 2, 5, 12, 33])
+    S = rng.choice([1, 1, 1, 2, 4, 9, 31, 64, 150, 333])
+    while groups * per * Hkv * R * S > 20000 and per > 1:
+        per //= 2
+    shared = [rng.choice([0, 16, 100, 512, 1500, 4200]) // page * page for _ in range(groups)]
+    causal = rng.random() < 0.5
+    least = S if causal and rng.random() < 0.7 else 0
+    lens = [shared[b // per] + least + rng.choice([0, 1, 17, 64, 130, 700, 2100])
+            for b in range(groups * per)]
+    q_len = [rng.randrange(0, S + 1) for _ in lens] if rng.random() < 0.4 else None
+    print(f"case random {seed}: {dtype} page={page} d={d} Hkv={Hkv} R={R} {groups}x{per} S={S} "
+          f"shared={shared} causal={causal} q_len={q_len is not None}", flush=True)
+    q, kp, vp, table = make(seed, lens, Hkv * R, Hkv, S, d, page, dtype, shared)
+    full = reference(q, kp, vp, table, lens, d ** -0.5, causal, q_len)
+    claim = rng.choice([shared, shared, [n // 2 for n in shared], None])
+    o, lse = check(q, kp, vp, table, lens, d ** -0.5, shared=claim, q_len=q_len, causal=causal,
+                   want=full)
+    again = check(q, kp, vp, table, lens, d ** -0.5, shared=claim, q_len=q_len, causal=causal,
+                  want=full)
+    assert torch.equal(o, again[0]) and torch.equal(lse, again[1]), "run to run"
