@@ -436,10 +436,11 @@ int sa_cache_indicator(const void* y_v, const void* y_v_hat,
  *                     -1 = none
  *   seq_len           [B] i32: tokens of each sequence (negative counts as 0)
  *   page_ref          [n_pages] i32: how many table entries name the page; 0 = free
- * page in {16, 32, 64, 128}; max_pages * page <= 2^30; B <= 16384 (the attention:
- * B + n_groups <= 1024, B * Hkv <= 65535).  Every list lives on the device, so the calls can be
- * captured into a HIP graph and follow the lists' values at each replay.  Calls
- * on one cache that may overlap in time must be ordered by the caller.
+ * page in {16, 32, 64, 128}; max_pages * page <= 2^30; B <= 16384 (the
+ * attention: B + n_groups <= 1024, B * Hkv <= 65535).  Every list lives on the
+ * device, so the calls can be captured into a HIP graph and follow the lists'
+ * values at each replay.  Calls on one cache that may overlap in time must be
+ * ordered by the caller.
  */
 
 /*
@@ -468,12 +469,15 @@ int sa_pages_reserve(int32_t* page_table, int32_t* seq_len, int32_t* page_ref,
  *   k, v       [B,Hkv,S,d] in dtype; not overlapping the pages
  *   n_new      [B] i32, at most S count; NULL = S for every sequence.  Rows from
  *              n_new[b] on are not read, and tokens without a page not written.
+ *   missing    [1] i32, nullable: what sa_pages_reserve returned for these tokens;
+ *              nothing is written unless it is 0 (the last n_new[b] tokens would
+ *              be older ones)
  */
 int sa_pages_write(const void* k, const void* v, void* k_pages, void* v_pages,
                    const int32_t* page_table, const int32_t* seq_len,
-                   const int32_t* n_new, int B, int Hkv, int S, int d,
-                   int dtype, int n_pages, int page, int max_pages,
-                   void* stream);
+                   const int32_t* n_new, const int32_t* missing, int B, int Hkv,
+                   int S, int d, int dtype, int n_pages, int page,
+                   int max_pages, void* stream);
 
 /*
  * sa_pages_fork -- sequence dst[i] becomes a copy of sequence src[i], i < n.
@@ -481,11 +485,12 @@ int sa_pages_write(const void* k, const void* v, void* k_pages, void* v_pages,
  * The full pages are shared (an owner more each).  A partial last page gets a
  * fresh page, so that both sequences can go on writing: the pair (copy_src[i],
  * copy_dst[i]) is to be copied in every pool with sa_pages_copy before either is
- * written; both are -1 where there is nothing to copy.  An entry whose src has
- * no tokens (or more than its table row), whose dst has some, or that names a sequence outside [0,B) is left
- * out, and of several entries with one dst the first counts.  Fresh pages are
- * the lowest free ones, in the order of the entries; with too few nothing is
- * changed, missing[0] is how many lack (otherwise 0), and all pairs are -1.
+ * written; both are -1 where there is nothing to copy.  An entry is left out if
+ * its src has no tokens or more than its table row has room for, if its dst has
+ * some, or if it names a sequence outside [0,B); of several entries with one dst
+ * the first counts.  Fresh pages are the lowest free ones, in the order of the
+ * entries; with too few nothing is changed, missing[0] is how many lack
+ * (otherwise 0), and all pairs are -1.
  *
  *   src, dst            [n] i32, 1 <= n <= B
  *   copy_src, copy_dst  [n] i32 out

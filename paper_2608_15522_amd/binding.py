@@ -54,8 +54,8 @@ SIGNATURES = {
     "sa_build_block_mask_pooled": (_I, [_VP, _VP, _I, _I, _I, _I, _F, _I, _I, _VP, _VP, _VP,
                                         _VP, _VP, _VP]),
     "sa_pages_reserve": (_I, [_VP, _VP, _VP, _VP, _I, _I, _I, _I, _VP, _VP]),
-    "sa_pages_write": (_I, [_VP, _VP, _VP, _VP, _VP, _VP, _VP, _I, _I, _I, _I, _I, _I, _I, _I,
-                            _VP]),
+    "sa_pages_write": (_I, [_VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _I, _I, _I, _I, _I, _I, _I,
+                            _I, _VP]),
     "sa_pages_fork": (_I, [_VP, _VP, _VP, _VP, _VP, _I, _I, _I, _I, _I, _VP, _VP, _VP, _VP]),
     "sa_pages_free": (_I, [_VP, _VP, _VP, _VP, _I, _I, _I, _I, _I, _VP]),
     "sa_pages_compact": (_I, [_VP, _VP, _I, _I, _I, _VP, _VP, _VP, _VP]),
@@ -541,9 +541,10 @@ def sa_pages_reserve(page_table, seq_len, page_ref, n_new, page, *, missing=None
     return missing
 
 
-def sa_pages_write(k, v, k_pages, v_pages, page_table, seq_len, *, n_new=None):
+def sa_pages_write(k, v, k_pages, v_pages, page_table, seq_len, *, n_new=None, missing=None):
     """The last n_new[b] tokens' rows of k, v [B,Hkv,S,d] into the pages
-    [n_pages,Hkv,page,d]; returns (k_pages, v_pages)."""
+    [n_pages,Hkv,page,d], unless missing [1] (what sa_pages_reserve returned for
+    them) is not 0; returns (k_pages, v_pages)."""
     B, Hkv, S, d = k.shape
     n_pages, _, page, _ = k_pages.shape
     _table(page_table, seq_len)
@@ -552,11 +553,12 @@ def sa_pages_write(k, v, k_pages, v_pages, page_table, seq_len, *, n_new=None):
     _expect(v_pages, "v_pages", (n_pages, Hkv, page, d), k.dtype)
     _expect(seq_len, "seq_len", (B,), torch.int32)
     _expect(n_new, "n_new", (B,), torch.int32)
-    _here(k, v, k_pages, v_pages, page_table, seq_len, n_new)
+    _expect(missing, "missing", (1,), torch.int32)
+    _here(k, v, k_pages, v_pages, page_table, seq_len, n_new, missing)
     _check(lib().sa_pages_write(
         _ptr(k), _ptr(v), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(seq_len),
-        _ptr(n_new), B, Hkv, S, d, _dtype_code(k), n_pages, page, page_table.shape[1],
-        _stream()))
+        _ptr(n_new), _ptr(missing), B, Hkv, S, d, _dtype_code(k), n_pages, page,
+        page_table.shape[1], _stream()))
     return k_pages, v_pages
 
 

@@ -292,9 +292,9 @@ void launch_pages_compact(int32_t* table, int32_t* ref, int B, int max_pages, in
 void launch_pages_copy(void* pools, int n_pools, int n_pages, size_t page_bytes,
                        const int32_t* src, const int32_t* dst, int n, hipStream_t s);
 void launch_pages_write(const void* k, const void* v, void* k_pages, void* v_pages,
-                        const int32_t* table, const int32_t* seq_len, const int32_t* n_new, int B,
-                        int Hkv, int S, int row_bytes, int max_pages, int n_pages, int page,
-                        hipStream_t s);
+                        const int32_t* table, const int32_t* seq_len, const int32_t* n_new,
+                        const int32_t* missing, int B, int Hkv, int S, int row_bytes,
+                        int max_pages, int n_pages, int page, hipStream_t s);
 
 // Attention over pages.  The arguments of sa_prefix_attention but for d, dtype, the
 // workspace and the stream.

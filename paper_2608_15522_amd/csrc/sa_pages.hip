@@ -485,8 +485,9 @@ __global__ void __launch_bounds__(256)
 pages_write_kernel(const char* __restrict__ k, const char* __restrict__ v,
                    char* __restrict__ k_pages, char* __restrict__ v_pages,
                    const int32_t* __restrict__ table, const int32_t* __restrict__ seq_len,
-                   const int32_t* __restrict__ n_new, int Hkv, int S, int log_cpr,
-                   unsigned rows, int max_pages, int n_pages, int lp) {
+                   const int32_t* __restrict__ n_new, const int32_t* __restrict__ missing,
+                   int Hkv, int S, int log_cpr, unsigned rows, int max_pages, int n_pages, int lp) {
+  const bool none = missing != nullptr && missing[0] != 0;  // read with the first length
   const size_t pieces = static_cast<size_t>(rows) << log_cpr;
   const size_t step = static_cast<size_t>(gridDim.x) * 256;
   for (size_t i = static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x; i < pieces; i += step) {
@@ -496,7 +497,7 @@ pages_write_kernel(const char* __restrict__ k, const char* __restrict__ v,
     const int n = n_new != nullptr ? min(n_new[b], S) : S;
     const long long pos = static_cast<long long>(seq_len[b]) - n + s;
     const long long j = pos >> lp;
-    if (static_cast<int>(s) >= n || pos < 0 || j >= max_pages) continue;
+    if (none || static_cast<int>(s) >= n || pos < 0 || j >= max_pages) continue;
     const int p = table[static_cast<size_t>(b) * max_pages + j];
     if (p < 0 || p >= n_pages) continue;
     const size_t to = ((((static_cast<size_t>(p) * Hkv + h) << lp) + (pos & ((1 << lp) - 1)))
@@ -568,9 +569,9 @@ void launch_pages_copy(void* pools, int n_pools, int n_pages, size_t page_bytes,
 }
 
 void launch_pages_write(const void* k, const void* v, void* k_pages, void* v_pages,
-                        const int32_t* table, const int32_t* seq_len, const int32_t* n_new, int B,
-                        int Hkv, int S, int row_bytes, int max_pages, int n_pages, int page,
-                        hipStream_t s) {
+                        const int32_t* table, const int32_t* seq_len, const int32_t* n_new,
+                        const int32_t* missing, int B, int Hkv, int S, int row_bytes,
+                        int max_pages, int n_pages, int page, hipStream_t s) {
   const unsigned rows = static_cast<unsigned>(B) * Hkv * S;
   const int log_cpr = log2_of(row_bytes / 16);
   const size_t wgs = ((static_cast<size_t>(rows) << log_cpr) + 255) / 256;
@@ -579,7 +580,7 @@ void launch_pages_write(const void* k, const void* v, void* k_pages, void* v_pag
                      dim3(static_cast<unsigned>(wgs < 8192 ? wgs : 8192)), dim3(256), 0, s,
                      static_cast<const char*>(k), static_cast<const char*>(v),
                      static_cast<char*>(k_pages), static_cast<char*>(v_pages), table, seq_len,
-                     n_new, Hkv, S, log_cpr, rows, max_pages, n_pages, log2_of(page));
+                     n_new, missing, Hkv, S, log_cpr, rows, max_pages, n_pages, log2_of(page));
 }
 
 }  // namespace sa

@@ -85,8 +85,8 @@ int sa_pages_reserve(int32_t* page_table, int32_t* seq_len, int32_t* page_ref,
 
 int sa_pages_write(const void* k, const void* v, void* k_pages, void* v_pages,
                    const int32_t* page_table, const int32_t* seq_len, const int32_t* n_new,
-                   int B, int Hkv, int S, int d, int dtype, int n_pages, int page, int max_pages,
-                   void* stream) {
+                   const int32_t* missing, int B, int Hkv, int S, int d, int dtype, int n_pages,
+                   int page, int max_pages, void* stream) {
   const char* fn = "sa_pages_write";
   SA_TRY(check_cache(fn, B, max_pages, n_pages, page, sa::kMaxSequences));
   SA_TRY(check_rows(fn, Hkv, S, d, dtype));
@@ -99,6 +99,7 @@ int sa_pages_write(const void* k, const void* v, void* k_pages, void* v_pages,
   SA_TRY(check_tensor(fn, "page_table", page_table, true, 4));
   SA_TRY(check_tensor(fn, "seq_len", seq_len, true, 4));
   SA_TRY(check_tensor(fn, "n_new", n_new, false, 4));
+  SA_TRY(check_tensor(fn, "missing", missing, false, 4));
   const int row_bytes = d * (dtype == SA_BF16 ? 2 : 4);
   const size_t rows = static_cast<size_t>(B) * Hkv * S * row_bytes;
   const size_t pool = static_cast<size_t>(n_pages) * Hkv * page * row_bytes;
@@ -107,8 +108,8 @@ int sa_pages_write(const void* k, const void* v, void* k_pages, void* v_pages,
   if (overlap(k, rows, k_pages, pool) || overlap(v, rows, k_pages, pool) ||
       overlap(k, rows, v_pages, pool) || overlap(v, rows, v_pages, pool))
     return fail(SA_ERR_INVALID_ARG, "%s: k or v overlaps the pages", fn);
-  sa::launch_pages_write(k, v, k_pages, v_pages, page_table, seq_len, n_new, B, Hkv, S, row_bytes,
-                         max_pages, n_pages, page, static_cast<hipStream_t>(stream));
+  sa::launch_pages_write(k, v, k_pages, v_pages, page_table, seq_len, n_new, missing, B, Hkv, S,
+                         row_bytes, max_pages, n_pages, page, static_cast<hipStream_t>(stream));
   return check_launch(fn);
 }
 

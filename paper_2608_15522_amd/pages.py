@@ -3,8 +3,9 @@
 ``KVPages`` allocates the pages of every layer and the lists that describe them once
 (with torch), as ``LayerPlan`` does for one layer of the sparse path; its methods enqueue
 the library's kernels on the current stream and never wait for the GPU.  What may fail
-for want of pages (``reserve``, ``fork``) says so in ``missing``, a device tensor that the
-caller reads when it likes.
+for want of pages (``reserve``, ``fork``) returns how many lack, a device tensor that the
+caller reads when it likes: until then a reservation that failed has changed nothing, and
+``write`` writes nothing.
 """
 from __future__ import annotations
 
@@ -17,7 +18,8 @@ class KVPages:
     """Pages for up to B sequences of at most max_tokens tokens, in ``layers`` layers.
 
     kv         [layers,2,n_pages,Hkv,page,d]: keys and values of every layer
-    page_table, seq_len, page_ref, missing: as the C calls document them
+    page_table, seq_len, page_ref: as the C calls document them
+    missing, fork_missing: [1] i32, of the last reserve and of the last fork
     """
 
     def __init__(self, B, max_tokens, n_pages, Hkv, d, page=64, layers=1,
@@ -26,7 +28,8 @@ class KVPages:
         e = lambda *s: torch.zeros(*s, dtype=torch.int32, device=device)
         self.kv = torch.empty(layers, 2, n_pages, Hkv, page, d, dtype=dtype, device=device)
         self.page_table = e(B, -(-max_tokens // page)).fill_(-1)
-        self.seq_len, self.page_ref, self.missing = e(B), e(n_pages), e(1)
+        self.seq_len, self.page_ref = e(B), e(n_pages)
+        self.missing, self.fork_missing = e(1), e(1)
         self._pools = self.kv.view(2 * layers, n_pages, Hkv, page, d)
 
     def reserve(self, n_new):
@@ -35,9 +38,9 @@ class KVPages:
                                    self.page, missing=self.missing)
 
     def write(self, layer, k, v, n_new=None):
-        """Keys and values [B,Hkv,S,d] of the tokens reserved last."""
+        """Keys and values [B,Hkv,S,d] of the tokens reserved last, if they were."""
         sa.sa_pages_write(k, v, self.kv[layer, 0], self.kv[layer, 1], self.page_table,
-                          self.seq_len, n_new=n_new)
+                          self.seq_len, n_new=n_new, missing=self.missing)
 
     def attend(self, layer, q, scale, **options):
         """sa_prefix_attention of q [B,Hq,S,d] over the layer's pages; returns (o, lse)."""
@@ -48,9 +51,9 @@ class KVPages:
         """Sequences dst (without tokens) become copies of sequences src; the pages that
         both would write are copied in every layer."""
         pairs = sa.sa_pages_fork(self.page_table, self.seq_len, self.page_ref, src, dst,
-                                 self.page, missing=self.missing)
+                                 self.page, missing=self.fork_missing)
         sa.sa_pages_copy(self._pools, pairs[0], pairs[1])
-        return self.missing
+        return self.fork_missing
 
     def free(self, seqs):
         """The sequences of seqs give up their pages."""

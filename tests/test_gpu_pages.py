@@ -198,6 +198,26 @@ def test_write_skips_tokens_without_a_page():
     assert torch.equal(vp, want)
 
 
+def test_write_behind_a_reservation_that_failed_writes_nothing():
+    """Two tokens fit behind fourteen, three do not: without its own room a write would go
+    over the last tokens that are there."""
+    t, n, r = ints([[1, -1], [0, -1]]), ints([14, 16]), ints([1, 1])
+    kp, vp = torch.ones(2, 1, 16, 64, device="cuda"), torch.ones(2, 1, 16, 64, device="cuda")
+    x = torch.full((2, 1, 3, 64), 5.0, device="cuda")
+    new = ints([3, 0])
+    missing = sa.sa_pages_reserve(t, n, r, new, 16)
+    sa.sa_pages_write(x, x, kp, vp, t, n, n_new=new, missing=missing)
+    assert missing.item() == 1 and n.tolist() == [14, 16]
+    assert (kp == 1).all() and (vp == 1).all()
+    new = ints([2, 0])
+    missing = sa.sa_pages_reserve(t, n, r, new, 16)
+    sa.sa_pages_write(x, x, kp, vp, t, n, n_new=new, missing=missing)
+    assert missing.item() == 0 and n.tolist() == [16, 16]
+    want = torch.ones_like(kp)
+    want[1, 0, 14:] = 5
+    assert torch.equal(kp, want) and torch.equal(vp, want)
+
+
 def test_offsets_past_32_bits():
     """Pools of over 4 GiB: the last pages are written, copied and read."""
     Hkv, page, d = 16, 128, 128
@@ -365,4 +385,15 @@ def test_pages_of_several_layers_through_the_class():
     assert counts[0].item() == (cache.page_ref > 0).sum().item()
     look(64)
     grow([5, 3, 0, 40])
+    look(64)
+    # a reservation that fails, and its writes, change nothing; a fork that fails neither
+    # hinders the next ones
+    m = ints([500, 0, 0, 0])  # a row has room for 13 pages of 32
+    assert cache.reserve(m).item() > 0
+    x = torch.full((B, Hkv, S, d), 9.0, device="cuda")
+    for layer in range(layers):
+        cache.write(layer, x, x, m)
+    look(64)
+    assert cache.fork(ints([1]), ints([3])).item() == 0  # 3 has tokens: left out
+    grow([1, 0, 2, 0])
     look(64)

@@ -31,8 +31,8 @@ _cache = dict(B=4, max_pages=8, n_pages=32, page=16)
 _reserve = Call("sa_pages_reserve", page_table=FAKE, seq_len=FAKE, page_ref=FAKE, n_new=FAKE,
                 **_cache, missing=FAKE, stream=None)
 _write = Call("sa_pages_write", k=FAR, v=FAR, k_pages=FAKE, v_pages=FARTHER, page_table=FAKE,
-              seq_len=FAKE, n_new=None, B=4, Hkv=2, S=3, d=64, dtype=0, n_pages=32, page=16,
-              max_pages=8, stream=None)
+              seq_len=FAKE, n_new=None, missing=None, B=4, Hkv=2, S=3, d=64, dtype=0, n_pages=32,
+              page=16, max_pages=8, stream=None)
 _fork = Call("sa_pages_fork", page_table=FAKE, seq_len=FAKE, page_ref=FAKE, src=FAKE, dst=FAKE,
              n=2, **_cache, copy_src=FAKE, copy_dst=FAKE, missing=FAKE, stream=None)
 _free = Call("sa_pages_free", page_table=FAKE, seq_len=FAKE, page_ref=FAKE, seqs=FAKE, n=2,
@@ -73,6 +73,7 @@ INVALID += [
     (_write, dict(k=None), ARG, "k is NULL"), (_write, dict(v=FAR + 4), ARG, "v is not 16"),
     (_write, dict(v_pages=FAKE + 4096), ARG, "k_pages and v_pages overlap"),
     (_write, dict(k=FAKE + 4096), ARG, "overlaps the pages"),
+    (_write, dict(missing=FAKE + 2), ARG, "missing is not 4"),
     (_write, dict(B=16384, Hkv=4096, S=64), UNS, "too large"),
     (_fork, dict(n=0), ARG, "n=0"), (_fork, dict(n=5), ARG, "n=5"),
     (_fork, dict(src=None), ARG, "src is NULL"), (_fork, dict(dst=None), ARG, "dst is NULL"),
@@ -168,6 +169,8 @@ def test_binding_refuses_mismatched_tensors():
         sa.sa_pages_write(kv, kv.float(), kp, kp, t, n)
     with pytest.raises(ValueError, match="seq_len"):
         sa.sa_pages_write(kv[:2], kv[:2], kp, kp, t, n)
+    with pytest.raises(ValueError, match="missing"):
+        sa.sa_pages_write(kv, kv, kp, kp, t, n, missing=two)
     with pytest.raises(TypeError, match="k_pages"):
         sa.sa_prefix_attention(q, kp.float(), kp, t, n, 1.0)
     with pytest.raises(ValueError, match="page_table"):
