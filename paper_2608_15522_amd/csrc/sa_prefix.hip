@@ -12,12 +12,13 @@
 // Segments.  Per key head: the shared keys of each group against the rows of all its
 // sequences (kShared; only where a sequence has few rows), then each sequence's other
 // keys against its own rows.  The rows of (sequence, key head) are its Hq / Hkv heads
-// times S queries, which lie one behind the other in Q.  A segment is row tiles times
-// 64-key tiles; all of them, head by head, laid end to end are the call's units of work,
-// cut into equal runs, one per workgroup slot of the chip.  The lengths are read on the
-// device, so a captured call follows them; every workgroup finds its run by the same
-// prefix sums over the segments.  A row tile that runs share leaves partial rows, which
-// prefix_combine_kernel joins in key order, so results do not depend on timing.
+// times S queries (in its own segment, the queries that it has), which lie one behind the
+// other in Q.  A segment is row tiles times 64-key tiles; all of them, head by head, laid
+// end to end are the call's units of work, cut into runs that differ by a unit at most, one
+// per workgroup slot of the chip, unless whole row tiles are better (plan_of).  The lengths
+// are read on the device, so a captured call follows them; every workgroup finds its run by
+// the same prefix sums over the segments.  A row tile that runs share leaves partial rows,
+// which prefix_combine_kernel joins in key order, so results do not depend on timing.
 #include <float.h>
 
 #include "sa_device.h"
@@ -63,13 +64,14 @@ struct Args {
   float inv_N, inv_S, inv_RS;
   int n_pages, lp, max_pages, causal;
   int TRp, TRo;               // rows of a row tile: shared segments, own segments
+  int lTRp, lTRo;             // their logarithms
   int TR;                     // the larger of the two: rows of a partial row tile's place
   int cp, co;                 // cost of a row tile: shared segments, own segments
   Log2Scale c;
   int* shared_out;            // [G] shared tokens that the call takes once
   int2* parts;                // [row tiles] first slot, parts (0: none, 1: the whole tile)
-  int nrtp, nrto;             // row tiles of a segment
-  float inv_nrtp, inv_nrto;
+  int nrtp, nrto;             // row tiles of a segment (an own one with S queries)
+  float inv_nrtp;
   float* full;                // [2][B * Hq * S][D] partial rows of whole row tiles
   float2* full_ml;            // [2][B * Hq * S]
   float* piece;               // [2 slots][TR][D] partial rows of shared row tiles
@@ -119,12 +121,18 @@ struct Schedule {
   int off[kSegs + 1];
   int wave_tot[kMaxWaves];
   int len[kSegs];
+  int nq[kSegs];  // queries
   int sh[kSegs / 2];
   int most;  // units of the longest row tile
 };
 
 __device__ __forceinline__ int row_units(int cost, int keys) {
   return cost + ceil_div(keys, kTile);
+}
+
+// Row tiles of a sequence with nq queries.
+__device__ __forceinline__ int own_tiles(const Args& a, int nq) {
+  return (a.R * nq + a.TRo - 1) >> a.lTRo;
 }
 
 template <int W>
@@ -135,11 +143,12 @@ __device__ void build_schedule(const Args& a, Schedule& s) {
   if (tid == 0) s.most = 0;
   __syncthreads();
   for (int b = tid; b < a.B; b += NT) {
-    const int len = seq_tokens(a, b);
+    const int len = seq_tokens(a, b), nq = seq_queries(a, b);
     s.len[b] = len;
+    s.nq[b] = nq;
     if (a.G == 0) atomicMax(&s.most, row_units(a.co, len));
     if (a.G > 0 && len > 0)
-      atomicMin(&s.sh[group_of(a, b)], a.causal ? max(min(len - seq_queries(a, b) + 1, len), 0) : len);
+      atomicMin(&s.sh[group_of(a, b)], a.causal ? max(min(len - nq + 1, len), 0) : len);
   }
   __syncthreads();
   if (a.G > 0) {
@@ -155,7 +164,8 @@ __device__ void build_schedule(const Args& a, Schedule& s) {
   auto units = [&](int i) {
     if (i < a.G) return s.sh[i] == 0 ? 0 : a.nrtp * row_units(a.cp, s.sh[i]);
     const int b = i - a.G;
-    return a.nrto * row_units(a.co, a.G > 0 ? max(s.len[b] - s.sh[group_of(a, b)], 0) : s.len[b]);
+    return own_tiles(a, s.nq[b]) *
+           row_units(a.co, a.G > 0 ? max(s.len[b] - s.sh[group_of(a, b)], 0) : s.len[b]);
   };
   int sum = 0;
   for (int i = i0; i < i1; ++i) sum += units(i);
@@ -183,7 +193,9 @@ __device__ void build_schedule(const Args& a, Schedule& s) {
 struct Job {
   int h;            // key head
   int b0;           // kShared: first sequence of the group; else the sequence
-  int rows;         // rows of the segment
+  int rows;         // rows of the segment: kShared RS a sequence, else nq a query head
+  int nq;           // not kShared: the sequence's queries
+  float inv_nq;
   int row0;         // first row of the tile
   int pos0, pos1;   // key positions of the segment
   const int32_t* pages;  // table row that they are read through
@@ -193,20 +205,29 @@ struct Job {
   int piece;        // place of the partial rows if not
 };
 
-// Row rho of a segment: sequence, row within (sequence, key head), whether the segment has
-// it, and whether it holds a query.
+// Row rho of a segment: sequence, row within (sequence, key head), query, whether the
+// segment has it, and whether it holds a query.
 struct Row {
-  int b, in;
+  int b, in, query;
   bool inside, real;
 };
 __device__ __forceinline__ Row row_of(const Args& a, const Job& j, int rho) {
   Row r;
   r.inside = rho < j.rows;
   rho = r.inside ? rho : j.rows - 1;
-  const int k = j.shared ? div_small(rho, a.RS, a.inv_RS) : 0;
-  r.b = j.b0 + k;
-  r.in = rho - k * a.RS;
-  r.real = r.inside && query_of(a, r.in) < seq_queries(a, r.b);
+  if (j.shared) {
+    const int k = div_small(rho, a.RS, a.inv_RS);
+    r.b = j.b0 + k;
+    r.in = rho - k * a.RS;
+    r.query = query_of(a, r.in);
+    r.real = r.inside && r.query < seq_queries(a, r.b);
+  } else {
+    const int head = div_small(rho, j.nq, j.inv_nq);
+    r.b = j.b0;
+    r.in = rho + head * (a.S - j.nq);
+    r.query = rho - head * j.nq;
+    r.real = r.inside;
+  }
   return r;
 }
 __device__ __forceinline__ size_t row_index(const Args& a, int h, const Row& r) {
@@ -276,8 +297,7 @@ __device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xC07F);
 // Last key position that a row sees, plus one.
 __device__ __forceinline__ int row_end(const Args& a, const Job& j, const Row& r) {
   if (!a.causal || j.shared) return j.pos1;
-  const int last = seq_tokens(a, r.b) - seq_queries(a, r.b) + query_of(a, r.in);
-  return min(j.pos1, last + 1);
+  return min(j.pos1, seq_tokens(a, r.b) - j.nq + r.query + 1);
 }
 
 __device__ __forceinline__ float natural_lse(float m, float l) {
@@ -583,10 +603,12 @@ __device__ void attend_many(const Args& a, const Job& j, char* lds) {
   int most = run1, least = run1;       // the furthest and the nearest end of the tile's rows
   if (a.causal && !j.shared) {
     const int last = min(j.row0 + kManyRows, j.rows) - 1;
-    const bool one = j.row0 / a.S == last / a.S;  // all of one head: consecutive queries
-    const int nq = seq_queries(a, j.b0), q0 = seq_tokens(a, j.b0) - nq + 1;
-    most = min(run1, q0 + min(one ? last % a.S : a.S - 1, nq - 1));
-    least = min(run1, q0 + (one ? j.row0 % a.S : 0));
+    const int h0 = uniform(div_small(j.row0, j.nq, j.inv_nq));
+    const int h1 = uniform(div_small(last, j.nq, j.inv_nq));
+    const bool one = h0 == h1;  // all of one head: consecutive queries
+    const int q0 = seq_tokens(a, j.b0) - j.nq + 1;
+    most = min(run1, q0 + (one ? last - h1 * j.nq : j.nq - 1));
+    least = min(run1, q0 + (one ? j.row0 - h0 * j.nq : 0));
   }
   PageCursor cur;  // from the same page in every wave, so that all find the same
   cur.start(a, j.pages, run0);
@@ -1093,9 +1115,10 @@ __device__ __forceinline__ Place place_of(const Args& a, const Schedule& s, int 
   p.seg = uniform(before) - 1;
   const bool shared = p.seg < a.G;
   const int units = uniform(s.off[p.seg + 1]) - uniform(s.off[p.seg]);
-  const int tiles = shared ? a.nrtp : a.nrto;
+  const int tiles = shared ? a.nrtp : own_tiles(a, uniform(s.nq[p.seg - a.G]));
   p.per = units;
-  if (tiles > 1) p.per = uniform(div_small(units, tiles, shared ? a.inv_nrtp : a.inv_nrto));
+  if (tiles > 1)
+    p.per = uniform(div_small(units, tiles, shared ? a.inv_nrtp : 1.f / static_cast<float>(tiles)));
   const int x = in - uniform(s.off[p.seg]);
   p.rt = uniform(div_small(x, p.per, 1.f / static_cast<float>(p.per)));
   p.k = x - p.rt * p.per;
@@ -1162,8 +1185,10 @@ prefix_attention_kernel(const Args a, Split split) {
     t = static_cast<int>(static_cast<long long>(nt) * xcd / kXcds);
     end = static_cast<int>(static_cast<long long>(nt) * (xcd + 1) / kXcds);
     rest = t + (end - t) / slots_xcd * slots_xcd;
-    if (rest + lane < end)
-      per_l = row_units(a.co, s.len[(rest + lane) % (a.B * a.nrto) % a.B]);
+    if (rest + lane < end) {
+      const int in = (rest + lane) % (a.B * a.nrto), b = in % a.B;
+      if (a.nrto - 1 - in / a.B < own_tiles(a, s.nq[b])) per_l = row_units(a.co, s.len[b]);
+    }
     upto = per_l;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -1229,7 +1254,9 @@ prefix_attention_kernel(const Args a, Split split) {
     if (j.shared) {
       j.b0 = p.seg * a.N;
       j.rows = a.N * a.RS;
-      j.row0 = p.rt * a.TRp;
+      j.row0 = p.rt << a.lTRp;
+      j.nq = 1;
+      j.inv_nq = 1.f;
       j.pos0 = 0;
       j.pos1 = uniform(s.sh[p.seg]);
       int rep = j.b0;  // the group's first sequence with a key
@@ -1239,8 +1266,11 @@ prefix_attention_kernel(const Args a, Split split) {
     } else {
       j.b0 = p.seg - a.G;
       const int len = whole ? seq_tokens(a, j.b0) : s.len[j.b0];
-      j.rows = a.RS;
-      j.row0 = p.rt * a.TRo;
+      j.nq = uniform(whole ? seq_queries(a, j.b0) : s.nq[j.b0]);
+      j.inv_nq = 1.f / static_cast<float>(j.nq);
+      j.rows = a.R * j.nq;
+      j.row0 = p.rt << a.lTRo;
+      if (j.row0 >= j.rows) continue;  // a row tile of rows that hold no query
       j.pos0 = uniform(a.G > 0 ? min(s.sh[group_of(a, j.b0)], len) : 0);
       j.pos1 = uniform(len);
       j.pages = a.table + static_cast<size_t>(j.b0) * a.max_pages;
@@ -1285,9 +1315,17 @@ prefix_combine_kernel(const Args a, int chunk) {
   const int b = blockIdx.z, h = blockIdx.y, pair = b * a.Hkv + h;
   const int first_row = blockIdx.x * chunk, last_row = min(first_row + chunk, a.RS);
   const int2* own = a.parts + a.G * a.Hkv * a.nrtp + pair * a.nrto;
-  // one row tile, and written already unless it is cut
-  if (a.G == 0 && chunk <= a.TRo && own[first_row / a.TRo].y <= 1) return;
   const int nq = seq_queries(a, b), len = a.seq_len[b];
+  if (nq == 0) return;
+  // row among those that hold a query (or the next one that does, or the last)
+  auto own_row = [&](int in) {
+    const int head = div_small(in, a.S, a.inv_S);
+    return min(head * nq + min(in - head * a.S, nq), a.R * nq - 1);
+  };
+  // two row tiles at most, and written already unless they are cut
+  if (a.G == 0 && chunk <= a.TRo && own[own_row(first_row) >> a.lTRo].y <= 1 &&
+      own[own_row(last_row - 1) >> a.lTRo].y <= 1)
+    return;
   const int g = a.G > 0 ? group_of(a, b) : 0;
   const bool shared = a.G > 0 && len > 0 && a.shared_out[g] > 0;
   const size_t rows = static_cast<size_t>(a.B) * a.Hkv * a.RS;
@@ -1295,9 +1333,10 @@ prefix_combine_kernel(const Args a, int chunk) {
     const int in = min(r0 + ra, a.RS - 1);
     const bool real = r0 + ra < last_row && query_of(a, in) < nq;
     const size_t row = static_cast<size_t>(pair) * a.RS + in;
-    const int2 po = own[in / a.TRo];
+    const int at_own = own_row(in);
+    const int2 po = own[at_own >> a.lTRo];
     const int rho = (b - g * a.N) * a.RS + in;  // among the group's rows
-    const int2 ps = shared ? a.parts[(g * a.Hkv + h) * a.nrtp + rho / a.TRp] : make_int2(0, 0);
+    const int2 ps = shared ? a.parts[(g * a.Hkv + h) * a.nrtp + (rho >> a.lTRp)] : make_int2(0, 0);
     const int np = ps.y + po.y;
     const bool mine = real && (a.G > 0 || po.y > 1);  // else it is written already
     float M = -FLT_MAX, den = 0.f;
@@ -1310,7 +1349,7 @@ prefix_combine_kernel(const Args a, int chunk) {
         const bool whole = p.y == 1;
         const size_t place = static_cast<size_t>(2) * (p.x + k) + (k == 0 ? 1 : 0);
         const size_t at = whole ? (of_shared ? 0 : rows) + row
-                                : place * a.TR + (of_shared ? rho % a.TRp : in % a.TRo);
+                                : place * a.TR + (of_shared ? rho & (a.TRp - 1) : at_own & (a.TRo - 1));
         *x = ldg_f32x4((whole ? a.full : a.piece) + at * D + 4 * c4);
         return (whole ? a.full_ml : a.piece_ml)[at];
       };
@@ -1441,6 +1480,8 @@ void launch_prefix_attention(const PrefixCall& p, int dtype, int d, char* ws, hi
   a.causal = p.causal;
   a.TRp = w.shared_rows;
   a.TRo = w.own_rows;
+  a.lTRp = __builtin_ctz(static_cast<unsigned>(a.TRp));
+  a.lTRo = __builtin_ctz(static_cast<unsigned>(a.TRo));
   a.TR = w.piece_rows;
   const auto cost = [&](int rows) { return rows == kManyRows ? 4 : 6; };
   a.cp = cost(a.TRp);
@@ -1451,7 +1492,6 @@ void launch_prefix_attention(const PrefixCall& p, int dtype, int d, char* ws, hi
   a.nrtp = w.groups > 0 ? ceil_div(a.N * a.RS, a.TRp) : 0;
   a.nrto = ceil_div(a.RS, a.TRo);
   a.inv_nrtp = a.nrtp > 0 ? 1.f / static_cast<float>(a.nrtp) : 0.f;
-  a.inv_nrto = 1.f / static_cast<float>(a.nrto);
   a.full = reinterpret_cast<float*>(ws + w.full);
   a.full_ml = reinterpret_cast<float2*>(ws + w.full_ml);
   a.piece = reinterpret_cast<float*>(ws + w.piece);
