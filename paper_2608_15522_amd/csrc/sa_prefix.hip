@@ -12,8 +12,9 @@
 // Segments.  Per key head: the shared keys of each group against the rows of all its
 // sequences (kShared; only where a sequence has few rows), then each sequence's other
 // keys against its own rows.  The rows of (sequence, key head) are its Hq / Hkv heads
-// times S queries (in its own segment, the queries that it has), which lie one behind the
-// other in Q.  A segment is row tiles times 64-key tiles; all of them, head by head, laid
+// times S queries, which lie one behind the other in Q; in its own segment they are taken
+// query by query, as many as it has, so that the rows of a tile see nearly the same keys
+// under a causal mask.  A segment is row tiles times 64-key tiles; all of them, head by head, laid
 // end to end are the call's units of work, cut into runs that differ by a unit at most, one
 // per workgroup slot of the chip, unless whole row tiles are better (plan_of).  The lengths
 // are read on the device, so a captured call follows them; every workgroup finds its run by
@@ -49,6 +50,23 @@ constexpr float kSlackWeight = 1.f / 256.f;  // 2^-kRescaleSlack
 constexpr int kSnap = 2;
 constexpr int kRunMin = 5;  // least units of a run
 
+// A divisor d that the host knows: with l the bits of d - 1 and m = 2^(31+l) / d rounded
+// down, plus 1, floor(x / d) = floor(x m / 2^(31+l)) for 0 <= x < 2^31, since m d exceeds
+// 2^(31+l) by at most 2^l.
+struct Div {
+  int d;
+  uint32_t m;
+  int l;
+  __device__ __forceinline__ int by(int x) const {
+    return static_cast<int>(__umulhi(static_cast<uint32_t>(x) << 1, m) >> l);
+  }
+};
+Div divisor(int d) {
+  int l = 0;
+  while ((1ll << l) < d) ++l;
+  return {d, static_cast<uint32_t>((1ull << (31 + l)) / static_cast<uint32_t>(d) + 1), l};
+}
+
 struct Args {
   const void* q;
   const void* kp;
@@ -61,7 +79,7 @@ struct Args {
   const int32_t* q_len;       // NULL: S queries each
   int B, G, N;                // sequences, groups (0: no shared segments), sequences a group
   int Hkv, R, S, RS;          // key heads, query heads a key head, queries, R * S
-  float inv_N, inv_S, inv_RS;
+  Div by_N, by_S, by_R, by_RS, by_B, by_tiles;  // by_tiles: B * nrto
   int n_pages, lp, max_pages, causal;
   int TRp, TRo;               // rows of a row tile: shared segments, own segments
   int lTRp, lTRo;             // their logarithms
@@ -70,6 +88,9 @@ struct Args {
   Log2Scale c;
   int* shared_out;            // [G] shared tokens that the call takes once
   int2* parts;                // [row tiles] first slot, parts (0: none, 1: the whole tile)
+  int cols;                   // XCDs that share a head's row tiles (tile_of)
+  int longer;                 // of these, those that take by_longer.d row tiles; the others
+  Div by_longer, by_least;    // by_least.d
   int nrtp, nrto;             // row tiles of a segment (an own one with S queries)
   float inv_nrtp;
   float* full;                // [2][B * Hq * S][D] partial rows of whole row tiles
@@ -99,10 +120,10 @@ __device__ __forceinline__ int div_small(int x, int y, float inv) {
   return q;
 }
 
-__device__ __forceinline__ int group_of(const Args& a, int b) { return div_small(b, a.N, a.inv_N); }
-// Query of a row within (sequence, key head).
+__device__ __forceinline__ int group_of(const Args& a, int b) { return a.by_N.by(b); }
+// Query of a row within (sequence, key head), as they lie in Q.
 __device__ __forceinline__ int query_of(const Args& a, int in) {
-  return in - div_small(in, a.S, a.inv_S) * a.S;
+  return in - a.by_S.by(in) * a.S;
 }
 
 // An address that is the same in every lane, as the copies need it, for certain.
@@ -118,7 +139,7 @@ __device__ __forceinline__ const P* uniform(const P* p) {
 // tokens of each group: whole pages, at most what every sequence with a key has and
 // (causal) what its first query sees.
 struct Schedule {
-  int off[kSegs + 1];
+  alignas(16) int off[kSegs + 1];
   int wave_tot[kMaxWaves];
   int len[kSegs];
   int nq[kSegs];  // queries
@@ -130,28 +151,32 @@ __device__ __forceinline__ int row_units(int cost, int keys) {
   return cost + ceil_div(keys, kTile);
 }
 
-// Row tiles of a sequence with nq queries.
-__device__ __forceinline__ int own_tiles(const Args& a, int nq) {
-  return (a.R * nq + a.TRo - 1) >> a.lTRo;
+// Queries and row tiles of sequence b.
+__device__ __forceinline__ int queries_of(const Args& a, const Schedule& s, int b) {
+  return a.q_len == nullptr ? a.S : s.nq[b];
+}
+__device__ __forceinline__ int own_tiles(const Args& a, const Schedule& s, int b) {
+  return a.q_len == nullptr ? a.nrto : (a.R * s.nq[b] + a.TRo - 1) >> a.lTRo;
 }
 
-template <int W>
+template <int W, bool GROUPS>
 __device__ void build_schedule(const Args& a, Schedule& s) {
   constexpr int NT = W * kWave;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  for (int g = tid; g < a.G; g += NT) s.sh[g] = 0x7fffffff;
+  if constexpr (GROUPS)
+    for (int g = tid; g < a.G; g += NT) s.sh[g] = 0x7fffffff;
   if (tid == 0) s.most = 0;
   __syncthreads();
   for (int b = tid; b < a.B; b += NT) {
     const int len = seq_tokens(a, b), nq = seq_queries(a, b);
     s.len[b] = len;
     s.nq[b] = nq;
-    if (a.G == 0) atomicMax(&s.most, row_units(a.co, len));
-    if (a.G > 0 && len > 0)
+    if (!GROUPS) atomicMax(&s.most, row_units(a.co, len));
+    if (GROUPS && len > 0)
       atomicMin(&s.sh[group_of(a, b)], a.causal ? max(min(len - nq + 1, len), 0) : len);
   }
   __syncthreads();
-  if (a.G > 0) {
+  if constexpr (GROUPS) {
     for (int g = tid; g < a.G; g += NT) {
       // no sequence of the group has a key: nothing to share
       const int v = s.sh[g] == 0x7fffffff ? 0 : min(s.sh[g], max(a.shared_len[g], 0));
@@ -159,13 +184,13 @@ __device__ void build_schedule(const Args& a, Schedule& s) {
     }
     __syncthreads();
   }
-  const int n = a.G + a.B, each = ceil_div(n, NT);
+  const int groups = GROUPS ? a.G : 0, n = groups + a.B, each = ceil_div(n, NT);
   const int i0 = min(tid * each, n), i1 = min(i0 + each, n);
   auto units = [&](int i) {
-    if (i < a.G) return s.sh[i] == 0 ? 0 : a.nrtp * row_units(a.cp, s.sh[i]);
-    const int b = i - a.G;
-    return own_tiles(a, s.nq[b]) *
-           row_units(a.co, a.G > 0 ? max(s.len[b] - s.sh[group_of(a, b)], 0) : s.len[b]);
+    if (i < groups) return s.sh[i] == 0 ? 0 : a.nrtp * row_units(a.cp, s.sh[i]);
+    const int b = i - groups;
+    return own_tiles(a, s, b) *
+           row_units(a.co, GROUPS ? max(s.len[b] - s.sh[group_of(a, b)], 0) : s.len[b]);
   };
   int sum = 0;
   for (int i = i0; i < i1; ++i) sum += units(i);
@@ -193,9 +218,8 @@ __device__ void build_schedule(const Args& a, Schedule& s) {
 struct Job {
   int h;            // key head
   int b0;           // kShared: first sequence of the group; else the sequence
-  int rows;         // rows of the segment: kShared RS a sequence, else nq a query head
+  int rows;         // rows of the segment: kShared RS a sequence, else R a query
   int nq;           // not kShared: the sequence's queries
-  float inv_nq;
   int row0;         // first row of the tile
   int pos0, pos1;   // key positions of the segment
   const int32_t* pages;  // table row that they are read through
@@ -216,16 +240,15 @@ __device__ __forceinline__ Row row_of(const Args& a, const Job& j, int rho) {
   r.inside = rho < j.rows;
   rho = r.inside ? rho : j.rows - 1;
   if (j.shared) {
-    const int k = div_small(rho, a.RS, a.inv_RS);
+    const int k = a.by_RS.by(rho);
     r.b = j.b0 + k;
     r.in = rho - k * a.RS;
     r.query = query_of(a, r.in);
     r.real = r.inside && r.query < seq_queries(a, r.b);
   } else {
-    const int head = div_small(rho, j.nq, j.inv_nq);
     r.b = j.b0;
-    r.in = rho + head * (a.S - j.nq);
-    r.query = rho - head * j.nq;
+    r.query = a.by_R.by(rho);
+    r.in = (rho - r.query * a.R) * a.S + r.query;
     r.real = r.inside;
   }
   return r;
@@ -602,13 +625,9 @@ __device__ void attend_many(const Args& a, const Job& j, char* lds) {
   const int run0 = j.pos0 + kTile * j.t0, run1 = min(j.pos1, j.pos0 + kTile * j.t1);
   int most = run1, least = run1;       // the furthest and the nearest end of the tile's rows
   if (a.causal && !j.shared) {
-    const int last = min(j.row0 + kManyRows, j.rows) - 1;
-    const int h0 = uniform(div_small(j.row0, j.nq, j.inv_nq));
-    const int h1 = uniform(div_small(last, j.nq, j.inv_nq));
-    const bool one = h0 == h1;  // all of one head: consecutive queries
-    const int q0 = seq_tokens(a, j.b0) - j.nq + 1;
-    most = min(run1, q0 + (one ? last - h1 * j.nq : j.nq - 1));
-    least = min(run1, q0 + (one ? j.row0 - h0 * j.nq : 0));
+    const int q0 = seq_tokens(a, j.b0) - j.nq + 1, last = min(j.row0 + kManyRows, j.rows) - 1;
+    most = min(run1, q0 + a.by_R.by(last));
+    least = min(run1, q0 + a.by_R.by(j.row0));
   }
   PageCursor cur;  // from the same page in every wave, so that all find the same
   cur.start(a, j.pages, run0);
@@ -1104,18 +1123,19 @@ __device__ __forceinline__ bool cuts(int cost, int per, int k) {
 struct Place {
   int h, seg, rt, k, per;
 };
+template <bool GROUPS>
 __device__ __forceinline__ Place place_of(const Args& a, const Schedule& s, int per_head,
                                           float inv_head, int u) {
-  const int lane = threadIdx.x & 63, n = a.G + a.B;
+  const int lane = threadIdx.x & 63, groups = GROUPS ? a.G : 0, n = groups + a.B;
   Place p;
   p.h = uniform(div_small(u, per_head, inv_head));
   const int in = u - p.h * per_head;
   int before = 0;  // segments that start at or before `in`: the last of them is not empty
   for (int i = 0; i < n; i += 64) before += __popcll(__ballot(i + lane < n && s.off[i + lane] <= in));
   p.seg = uniform(before) - 1;
-  const bool shared = p.seg < a.G;
+  const bool shared = p.seg < groups;
   const int units = uniform(s.off[p.seg + 1]) - uniform(s.off[p.seg]);
-  const int tiles = shared ? a.nrtp : own_tiles(a, uniform(s.nq[p.seg - a.G]));
+  const int tiles = shared ? a.nrtp : a.nrto == 1 ? 1 : uniform(own_tiles(a, s, p.seg - groups));
   p.per = units;
   if (tiles > 1)
     p.per = uniform(div_small(units, tiles, shared ? a.inv_nrtp : 1.f / static_cast<float>(tiles)));
@@ -1125,35 +1145,83 @@ __device__ __forceinline__ Place place_of(const Args& a, const Schedule& s, int 
   return p;
 }
 
-// How the row tiles reach the workgroups: kRuns as above; kWhole one row tile a workgroup,
-// every one written out at once.  In kRuns, if no sequence's rows take much longer than the
-// mean and there are as many row tiles as slots, each slot first takes whole row tiles, in
-// rounds of all slots of an XCD, and only the rest is cut (kRounds): the workgroups of a
-// round go through a head's keys side by side, so that these come from the XCD's L2.  16
+// How the row tiles reach the workgroups.  kWhole: one row tile a workgroup, every one
+// written out at once.  kRuns: as above, without shared segments; if no sequence's rows take
+// much longer than the mean and there are as many row tiles as slots, each slot first takes
+// whole row tiles, in rounds of all slots of an XCD, and only the rest is cut: the workgroups
+// of a round go through a head's keys side by side, so that these come from the XCD's L2.  16
 // heads of 4 x 1024 queries over 16000 keys (a whole row tile a slot) run at 920 TFLOP/s, 20
-// heads cut into equal runs at 740.
-enum Split { kRuns, kWhole };
+// heads cut into equal runs at 740.  kGroups: runs over shared and own segments.  Each is a
+// kernel of its own, since a short call waits for its instructions as long as for its data: 4
+// sequences of 316 tokens, 8 heads of d 64, 6.4 us in a kernel of kWhole alone, 7.8 in one of
+// all three.
+enum Split { kWhole, kRuns, kGroups };
 
 // Row tile t of a call without shared segments: head by head, the last rows first (under a
-// causal mask they see the most keys), sequence by sequence.
+// causal mask they see the most keys), sequence by sequence.  With a.cols > 1 XCDs to a head
+// (kWhole) each takes every a.cols-th row tile, so that they have as many keys to see.
 struct Tile {
   int h, b, rt;
 };
+template <bool WHOLE>
 __device__ __forceinline__ Tile tile_of(const Args& a, int t) {
-  const int per = a.B * a.nrto;
   Tile x;
-  x.h = uniform(t / per);
-  const int in = t - x.h * per, q = uniform(in / a.B);
-  x.rt = a.nrto - 1 - q;
+  x.h = a.by_tiles.by(t);
+  const int in = t - x.h * a.by_tiles.d;
+  int q = a.by_B.by(in);
   x.b = in - q * a.B;
+  if (WHOLE && a.cols > 1) {
+    const int cut = a.longer * a.by_longer.d;
+    if (q < cut) {
+      const int c = a.by_longer.by(q);
+      q = (q - c * a.by_longer.d) * a.cols + c;
+    } else {
+      const int c = a.by_least.by(q - cut);
+      q = (q - cut - c * a.by_least.d) * a.cols + c + a.longer;
+    }
+  }
+  x.rt = a.nrto - 1 - q;
   return x;
+}
+
+// In kWhole a CU has one or two row tiles at a time, so the longest ones decide.  An XCD's row
+// tiles are ranked by the keys that they see, the most first, and the second half of those
+// that run together the other way round: its longest one shares its CU with its shortest.
+// Returns this workgroup's tile of [t0, t0 + n).
+constexpr int kCusXcd = 32;
+template <int W>
+__device__ int ranked_tile(const Args& a, Schedule& s, int t0, int n, int in_xcd) {
+  const int i = threadIdx.x;
+  uint32_t mine = 0;
+  if (i < n) {
+    const Tile x = tile_of<true>(a, t0 + i);
+    const int nq = seq_queries(a, x.b), row0 = x.rt << a.lTRo, rows = a.R * nq;
+    int keys = row0 < rows ? seq_tokens(a, x.b) : 0;
+    if (a.causal && row0 < rows) {
+      const int last = min(row0 + a.TRo, rows) - 1;
+      keys = max(keys - nq + a.by_R.by(last) + 1, 0);
+    }
+    mine = static_cast<uint32_t>(ceil_div(keys, kTile)) << 8 | static_cast<uint32_t>(255 - i);
+  }
+  uint32_t* all = reinterpret_cast<uint32_t*>(s.off);
+  if (i < 256) all[i] = mine;
+  __syncthreads();
+  int rank = 0;
+  for (int k = 0; k < n; k += 4) {
+    const u32x4 x = *reinterpret_cast<const u32x4*>(all + k);
+    rank += (x.x > mine) + (x.y > mine) + (x.z > mine) + (x.w > mine);
+  }
+  if (i < n) s.len[rank] = t0 + i;
+  __syncthreads();
+  const int first = min(n, 2 * kCusXcd);
+  return s.len[in_xcd < kCusXcd || in_xcd >= first ? in_xcd : first - 1 - (in_xcd - kCusXcd)];
 }
 
 // W waves a workgroup: with eight, two workgroups' worth of buffers and waves work on one
 // row tile.
-template <int D, typename T, bool MANY_SHARED, bool MANY_OWN, int W>
+template <int D, typename T, bool MANY_SHARED, bool MANY_OWN, int W, Split SPLIT>
 __global__ void __launch_bounds__(W * kWave) __attribute__((amdgpu_waves_per_eu(2, 2)))
-prefix_attention_kernel(const Args a, Split split) {
+prefix_attention_kernel(const Args a) {
   static_assert(W == 4 || !(MANY_SHARED || MANY_OWN), "the form of many rows has four waves");
   __shared__ __attribute__((aligned(1024))) char lds[attend_lds<D, W>()];
   __shared__ float2 lds_ml[W * kJoinRows];
@@ -1163,31 +1231,41 @@ prefix_attention_kernel(const Args a, Split split) {
   // consecutive runs on one XCD, so that row tiles of a head share their keys in its L2
   const int slot = xcd * slots_xcd + in_xcd;
   const int nt = a.Hkv * a.B * a.nrto;
-  const bool whole = split == kWhole;
+  constexpr bool whole = SPLIT == kWhole, GROUPS = SPLIT == kGroups;
+  const int groups = GROUPS ? a.G : 0;
   bool rounds = false;
   int per_head = 1, total = 0;
   float inv_head = 1.f;
-  if (!whole) {
-    build_schedule<W>(a, s);
-    per_head = uniform(s.off[a.G + a.B]);
+  if constexpr (!whole) {
+    build_schedule<W, GROUPS>(a, s);
+    per_head = uniform(s.off[groups + a.B]);
     total = per_head * a.Hkv;
     inv_head = 1.f / static_cast<float>(per_head);
-    if (blockIdx.x == 0)
-      for (int i = threadIdx.x; i < a.G; i += W * kWave) a.shared_out[i] = s.sh[i];
-    rounds = a.G == 0 && nt >= static_cast<int>(gridDim.x) &&
-             uniform(s.most) <= 1.25f * static_cast<float>(total) / static_cast<float>(nt);
+    if constexpr (GROUPS) {
+      if (blockIdx.x == 0)
+        for (int i = threadIdx.x; i < a.G; i += W * kWave) a.shared_out[i] = s.sh[i];
+    } else {
+      rounds = nt >= static_cast<int>(gridDim.x) &&
+               uniform(s.most) <= 1.25f * static_cast<float>(total) / static_cast<float>(nt);
+    }
   }
   // Rounds: row tiles [t, end) of the XCD, slots_xcd at a time.  What remains then, less than
   // one row tile a slot, is kept a row tile a lane (slots_xcd is 64): units `per_l`, `upto`
   // with those of the lanes before.
   int t = slot, end = nt, rest = 0, per_l = 0, upto = 0;
+  if constexpr (whole) {
+    const int n = min(slots_xcd, nt - xcd * slots_xcd);
+    if (in_xcd >= n) return;
+    if (n > kCusXcd && n <= 256)
+      t = uniform(ranked_tile<W>(a, s, xcd * slots_xcd, n, in_xcd));
+  }
   if (rounds) {
     t = static_cast<int>(static_cast<long long>(nt) * xcd / kXcds);
     end = static_cast<int>(static_cast<long long>(nt) * (xcd + 1) / kXcds);
     rest = t + (end - t) / slots_xcd * slots_xcd;
     if (rest + lane < end) {
-      const int in = (rest + lane) % (a.B * a.nrto), b = in % a.B;
-      if (a.nrto - 1 - in / a.B < own_tiles(a, s.nq[b])) per_l = row_units(a.co, s.len[b]);
+      const Tile x = tile_of<whole>(a, rest + lane);
+      if (x.rt < own_tiles(a, s, x.b)) per_l = row_units(a.co, s.len[x.b]);
     }
     upto = per_l;
 #pragma unroll
@@ -1211,9 +1289,9 @@ prefix_attention_kernel(const Args a, Split split) {
   for (;; ++turn) {
     Place p;
     int take = 0, last = 0;  // slots behind this one that hold parts of a row tile begun here
-    if (turn >= 2 && t < (rounds ? rest : whole ? end : 0)) {
-      const Tile x = tile_of(a, t);
-      p = Place{x.h, a.G + x.b, x.rt, 0, row_units(a.co, whole ? 0 : s.len[x.b])};
+    if (!GROUPS && turn >= 2 && t < (rounds ? rest : whole ? end : 0)) {
+      const Tile x = tile_of<whole>(a, uniform(t));
+      p = Place{x.h, x.b, x.rt, 0, row_units(a.co, whole ? 0 : s.len[x.b])};
       take = p.per;
       t = whole ? end : t + slots_xcd;
     } else {
@@ -1224,14 +1302,14 @@ prefix_attention_kernel(const Args a, Split split) {
         const int i = uniform(__popcll(__ballot(upto <= x)));
         p.per = __builtin_amdgcn_readlane(per_l, i);
         p.k = x - (__builtin_amdgcn_readlane(upto, i) - p.per);
-        const Tile y = tile_of(a, rest + i);
+        const Tile y = tile_of<whole>(a, rest + i);
         p.h = y.h;
         p.seg = y.b;
         p.rt = y.rt;
-      } else {
-        p = place_of(a, s, per_head, inv_head, x);
+      } else if constexpr (!whole) {
+        p = place_of<GROUPS>(a, s, per_head, inv_head, x);
       }
-      const int cost = p.seg < a.G ? a.cp : a.co;
+      const int cost = p.seg < groups ? a.cp : a.co;
       if (turn < 2) {
         int y = x;
         if (!cuts(cost, p.per, p.k)) y = p.k < cost + kSnap ? x - p.k : x - p.k + p.per;
@@ -1246,17 +1324,16 @@ prefix_attention_kernel(const Args a, Split split) {
       if (take < p.per && p.k == 0) last = run_at(runs, u + p.per - kSnap) - my;
       u += take;
     }
-    const int cost = p.seg < a.G ? a.cp : a.co;
+    const int cost = p.seg < groups ? a.cp : a.co;
     Job j;
     int tile;  // the row tile's number in `parts`
     j.h = p.h;
-    j.shared = p.seg < a.G;
-    if (j.shared) {
+    j.shared = p.seg < groups;
+    if (GROUPS && j.shared) {
       j.b0 = p.seg * a.N;
       j.rows = a.N * a.RS;
       j.row0 = p.rt << a.lTRp;
-      j.nq = 1;
-      j.inv_nq = 1.f;
+      j.nq = 0;
       j.pos0 = 0;
       j.pos1 = uniform(s.sh[p.seg]);
       int rep = j.b0;  // the group's first sequence with a key
@@ -1264,17 +1341,16 @@ prefix_attention_kernel(const Args a, Split split) {
       j.pages = a.table + static_cast<size_t>(uniform(rep)) * a.max_pages;
       tile = (p.seg * a.Hkv + p.h) * a.nrtp + p.rt;
     } else {
-      j.b0 = p.seg - a.G;
+      j.b0 = p.seg - groups;
       const int len = whole ? seq_tokens(a, j.b0) : s.len[j.b0];
-      j.nq = uniform(whole ? seq_queries(a, j.b0) : s.nq[j.b0]);
-      j.inv_nq = 1.f / static_cast<float>(j.nq);
+      j.nq = uniform(whole ? seq_queries(a, j.b0) : queries_of(a, s, j.b0));
       j.rows = a.R * j.nq;
       j.row0 = p.rt << a.lTRo;
       if (j.row0 >= j.rows) continue;  // a row tile of rows that hold no query
-      j.pos0 = uniform(a.G > 0 ? min(s.sh[group_of(a, j.b0)], len) : 0);
+      j.pos0 = GROUPS ? uniform(min(s.sh[group_of(a, j.b0)], len)) : 0;
       j.pos1 = uniform(len);
       j.pages = a.table + static_cast<size_t>(j.b0) * a.max_pages;
-      tile = a.G * a.Hkv * a.nrtp + (j.b0 * a.Hkv + p.h) * a.nrto + p.rt;
+      tile = groups * a.Hkv * a.nrtp + (j.b0 * a.Hkv + p.h) * a.nrto + p.rt;
     }
     j.t0 = uniform(max(p.k - cost, 0));
     j.t1 = uniform(whole ? ceil_div(j.pos1, kTile) : max(p.k + take - cost, 0));
@@ -1284,7 +1360,7 @@ prefix_attention_kernel(const Args a, Split split) {
       a.parts[tile] = make_int2(slot, j.pos1 == j.pos0 ? 0 : last + 1);
     if constexpr (sizeof(T) == 4) {
       attend_f32<D, W>(a, j, lds, lds_ml);
-    } else if constexpr (MANY_SHARED == MANY_OWN) {
+    } else if constexpr (MANY_SHARED == MANY_OWN || !GROUPS) {
       if constexpr (MANY_OWN)
         attend_many<D>(a, j, lds);
       else
@@ -1300,7 +1376,7 @@ prefix_attention_kernel(const Args a, Split split) {
 
 // Joins the partial rows of every row that has some: those of the shared keys, then those
 // of its own, in key order.  Workgroup (x, h, b) takes `chunk` rows of a (sequence, key
-// head); PG groups of D / 4 threads share a row, each taking every PG-th part, four parts'
+// head), in the order of its own segment; PG groups of D / 4 threads share a row, each taking every PG-th part, four parts'
 // loads at a time, and their sums are joined in group order.  Latency-bound: two loads in
 // turn.
 constexpr int kCombineThreads = 256;
@@ -1315,30 +1391,33 @@ prefix_combine_kernel(const Args a, int chunk) {
   const int b = blockIdx.z, h = blockIdx.y, pair = b * a.Hkv + h;
   const int first_row = blockIdx.x * chunk, last_row = min(first_row + chunk, a.RS);
   const int2* own = a.parts + a.G * a.Hkv * a.nrtp + pair * a.nrto;
-  const int nq = seq_queries(a, b), len = a.seq_len[b];
-  if (nq == 0) return;
-  // row among those that hold a query (or the next one that does, or the last)
-  auto own_row = [&](int in) {
-    const int head = div_small(in, a.S, a.inv_S);
-    return min(head * nq + min(in - head * a.S, nq), a.R * nq - 1);
-  };
-  // two row tiles at most, and written already unless they are cut
-  if (a.G == 0 && chunk <= a.TRo && own[own_row(first_row) >> a.lTRo].y <= 1 &&
-      own[own_row(last_row - 1) >> a.lTRo].y <= 1)
-    return;
+  // one row tile, and written already unless it is cut
+  if (a.G == 0 && chunk <= a.TRo && own[first_row >> a.lTRo].y <= 1) return;
+  // Three loads, pinned so that none waits for another; shared_out has any int without groups.
   const int g = a.G > 0 ? group_of(a, b) : 0;
-  const bool shared = a.G > 0 && len > 0 && a.shared_out[g] > 0;
+  int q_raw = (a.q_len != nullptr ? a.q_len : a.seq_len)[b], len = a.seq_len[b];
+  int taken = a.shared_out[g];
+  asm("" : "+s"(q_raw), "+s"(len), "+s"(taken));
+  const bool shared = a.G > 0 && len > 0 && taken > 0;
+  const int own_rows = a.R * (a.q_len != nullptr ? min(max(q_raw, 0), a.S) : a.S);
+  // What a part chooses between, pinned: the compiler would choose between the arguments'
+  // addresses and load the chosen one for each part, a latency of its own.
+  ptrdiff_t piece = a.piece - a.full, piece_ml = a.piece_ml - a.full_ml;
+  int mask_shared = a.TRp - 1, mask_own = a.TRo - 1;
+  asm("" : "+s"(piece), "+s"(piece_ml), "+s"(mask_shared), "+s"(mask_own));
   const size_t rows = static_cast<size_t>(a.B) * a.Hkv * a.RS;
   for (int r0 = first_row; r0 < last_row; r0 += RA) {
-    const int in = min(r0 + ra, a.RS - 1);
-    const bool real = r0 + ra < last_row && query_of(a, in) < nq;
+    const int at_own = min(r0 + ra, a.RS - 1);
+    const bool real = r0 + ra < last_row && at_own < own_rows;
+    const int query = a.by_R.by(at_own);
+    const int in = (at_own - query * a.R) * a.S + query;
     const size_t row = static_cast<size_t>(pair) * a.RS + in;
-    const int at_own = own_row(in);
     const int2 po = own[at_own >> a.lTRo];
     const int rho = (b - g * a.N) * a.RS + in;  // among the group's rows
     const int2 ps = shared ? a.parts[(g * a.Hkv + h) * a.nrtp + (rho >> a.lTRp)] : make_int2(0, 0);
     const int np = ps.y + po.y;
     const bool mine = real && (a.G > 0 || po.y > 1);  // else it is written already
+    const int in_shared = rho & mask_shared, in_own = at_own & mask_own;
     float M = -FLT_MAX, den = 0.f;
     f32x4 num = {0.f, 0.f, 0.f, 0.f};
     if (mine) {
@@ -1349,9 +1428,9 @@ prefix_combine_kernel(const Args a, int chunk) {
         const bool whole = p.y == 1;
         const size_t place = static_cast<size_t>(2) * (p.x + k) + (k == 0 ? 1 : 0);
         const size_t at = whole ? (of_shared ? 0 : rows) + row
-                                : place * a.TR + (of_shared ? rho & (a.TRp - 1) : at_own & (a.TRo - 1));
-        *x = ldg_f32x4((whole ? a.full : a.piece) + at * D + 4 * c4);
-        return (whole ? a.full_ml : a.piece_ml)[at];
+                                : place * a.TR + (of_shared ? in_shared : in_own);
+        *x = ldg_f32x4(a.full + (whole ? 0 : piece) + at * D + 4 * c4);
+        return a.full_ml[(whole ? 0 : piece_ml) + at];
       };
       for (int i0 = pg; i0 < np; i0 += 4 * PG) {
         f32x4 x[4];
@@ -1447,7 +1526,7 @@ Plan plan_of(const Args& a, const PrefixCall& p, bool bf16, int d) {
   const bool eight =
       few && (whole ? tiles <= kPrefixSlots / 2
                     : tiles <= 64 || (row >= 256 && (tiles <= kPrefixSlots / 2 || keys > 1024)));
-  return {whole ? kWhole : kRuns, eight ? 8 : 4};
+  return {whole ? kWhole : a.G > 0 ? kGroups : kRuns, eight ? 8 : 4};
 }
 
 }  // namespace
@@ -1471,9 +1550,10 @@ void launch_prefix_attention(const PrefixCall& p, int dtype, int d, char* ws, hi
   a.R = p.Hq / p.Hkv;
   a.S = p.S;
   a.RS = a.R * p.S;
-  a.inv_N = a.N > 0 ? 1.f / static_cast<float>(a.N) : 0.f;
-  a.inv_S = 1.f / static_cast<float>(a.S);
-  a.inv_RS = 1.f / static_cast<float>(a.RS);
+  a.by_N = divisor(a.N > 0 ? a.N : 1);
+  a.by_S = divisor(a.S);
+  a.by_R = divisor(a.R);
+  a.by_RS = divisor(a.RS);
   a.n_pages = p.n_pages;
   a.lp = __builtin_ctz(static_cast<unsigned>(p.page));
   a.max_pages = p.max_pages;
@@ -1492,6 +1572,8 @@ void launch_prefix_attention(const PrefixCall& p, int dtype, int d, char* ws, hi
   a.nrtp = w.groups > 0 ? ceil_div(a.N * a.RS, a.TRp) : 0;
   a.nrto = ceil_div(a.RS, a.TRo);
   a.inv_nrtp = a.nrtp > 0 ? 1.f / static_cast<float>(a.nrtp) : 0.f;
+  a.by_B = divisor(a.B);
+  a.by_tiles = divisor(a.B * a.nrto);
   a.full = reinterpret_cast<float*>(ws + w.full);
   a.full_ml = reinterpret_cast<float2*>(ws + w.full_ml);
   a.piece = reinterpret_cast<float*>(ws + w.piece);
@@ -1508,13 +1590,25 @@ void launch_prefix_attention(const PrefixCall& p, int dtype, int d, char* ws, hi
   const Split split = plan.split;
   const bool wide = plan.waves == 8;
   if (split == kWhole) a.G = 0;
+  a.cols = split == kWhole && a.Hkv < kXcds ? ceil_div(kXcds, a.Hkv) : 1;
+  a.longer = a.nrto % a.cols;
+  a.by_longer = divisor(a.nrto / a.cols + 1);
+  a.by_least = divisor(a.nrto >= a.cols ? a.nrto / a.cols : 1);
   const int slots = wide ? kPrefixSlots / 2 : kPrefixSlots;
   const int wgs = split == kWhole ? kXcds * ceil_div(a.Hkv * a.B * a.nrto, kXcds) : slots;
 #define SA_PREFIX(D, T, P, O, W)                                                              \
   do {                                                                                        \
-    hipLaunchKernelGGL((prefix_attention_kernel<D, T, P, O, W>), dim3(wgs), dim3(W * kWave), 0, \
-                       s, a, split);                                                          \
-    if (split == kWhole) break;                                                               \
+    if (split == kWhole) {                                                                    \
+      hipLaunchKernelGGL((prefix_attention_kernel<D, T, O, O, W, kWhole>), dim3(wgs),         \
+                         dim3(W * kWave), 0, s, a);                                           \
+      break;                                                                                  \
+    }                                                                                         \
+    if (split == kRuns)                                                                       \
+      hipLaunchKernelGGL((prefix_attention_kernel<D, T, O, O, W, kRuns>), dim3(wgs),          \
+                         dim3(W * kWave), 0, s, a);                                           \
+    else                                                                                      \
+      hipLaunchKernelGGL((prefix_attention_kernel<D, T, P, O, W, kGroups>), dim3(wgs),        \
+                         dim3(W * kWave), 0, s, a);                                           \
     if (share)                                                                                \
       hipLaunchKernelGGL((prefix_combine_kernel<D, T, 8>), cgrid, dim3(kCombineThreads), 0, s, \
                          a, chunk);                                                           \
@@ -1532,7 +1626,7 @@ void launch_prefix_attention(const PrefixCall& p, int dtype, int d, char* ws, hi
       SA_PREFIX(D, uint16_t, false, false, 8);  \
     else if (a.TRo == kManyRows)                \
       SA_PREFIX(D, uint16_t, true, true, 4);    \
-    else if (a.TRp == kManyRows && a.G > 0)     \
+    else if (a.TRp == kManyRows)                \
       SA_PREFIX(D, uint16_t, true, false, 4);   \
     else                                        \
       SA_PREFIX(D, uint16_t, false, false, 4);  \
