@@ -1503,16 +1503,20 @@ Plan plan_of(const Args& a, const PrefixCall& p, bool bf16, int d) {
     whole = bf16 ? keys <= 2048 && tiles * keys <= 1 << 20
                  : keys * d <= 1 << 17 && tiles * keys * d <= 1 << 25;
   } else if (many_own) {
-    // 48 row tiles of 144 rows at d 128: 16 against 21 us with room for 1000 keys, 27 against
-    // 24 with room for 2000.  Under a causal mask, where the queries are a quarter of a
-    // sequence's tokens or more, its row tiles see unequally many keys: 32 heads over 8, 1500
-    // queries, 81 against 101 us (96 row tiles: 39 against 48), 4000 queries of 8 heads (256
-    // row tiles of d 64) 65 against 58, of 32 heads 200 against 199.  Runs by the keys that
-    // each row tile sees took 67 and 64 us in the first and third of these, and up to twice
-    // as long as whole row tiles with fewer queries: they leave a head's keys to be read by
-    // workgroups at different places.
-    whole = keys <= 1024 || (tiles >= kPrefixSlots && keys <= 2048) ||
-            (p.causal && keys <= 4ll * p.S && (tiles >= kPrefixSlots || keys <= 4096));
+    // 2048 queries at d 128, whole against runs (us): a workgroup that is alone on its CU goes
+    // through its keys at half the card's rate, one of several rounds waits for the longest of
+    // each, and runs cost some 20 us of their own and read a head's keys at different places.
+    //   row tiles             128        256        384        640
+    //   2048 keys           36   43    42   59    60   79   104  105
+    //   4096                65   56    75   87   106  120   195  177
+    //   8192               123   84   140  143   200  206   385  318
+    //   causal, 4096        67   52    73   82    93  110   148  160
+    //   causal, 8192       124   79   139  138   187  198   332  300
+    // and 16 to 64 row tiles of 256 rows 28 to 29 against 30 to 35 with 1500 keys, 34 to 36
+    // against 30 to 36 with 2000.
+    whole = keys <= 1536 || (tiles >= kPrefixSlots / 4 && keys <= 2048) ||
+            (tiles >= kPrefixSlots / 2 && (p.causal ? keys <= 4096 || keys <= 2ll * p.S
+                                                    : keys <= 4096 && tiles <= kPrefixSlots));
   } else if (tiles <= kPrefixSlots / 2) {
     whole = bf16 ? keys <= 2048 : keys * d <= 1 << 16;
   } else {
