@@ -45,8 +45,8 @@ constexpr float kSlackWeight = 1.f / 256.f;  // 2^-kRescaleSlack
 // whatever its keys (finding its pages, the first copies' latency, its epilogue).  A cut
 // leaves at least kSnap tiles on either side, or moves to the row tile's end.  64 samples
 // of 4 query heads a key head (8 of them) over 16384 shared tokens and up to 2000 of their
-// own at d 128 take 113 us with costs of 4 (128 rows) and 6 (32 rows), 125 to 131 with tiles
-// of the 32-row form at twice the other's, 114 the other way round.
+// own at d 128 take 86 us with costs of 4 (128 rows) and 6 (32 rows), 83 to 87 with 2 to 4 of
+// either; 4 groups of 8 such samples 87, and 89 to 92.
 constexpr int kSnap = 2;
 constexpr int kRunMin = 5;  // least units of a run
 
@@ -463,18 +463,21 @@ __device__ void attend_few(const Args& a, const Job& j, char* lds_all, float2* l
   };
   // Own keys behind shared ones are read once, by this job, and leave the caches to the
   // shared ones (nt): 64 samples of 4 query heads over 16384 shared tokens and up to 2000 of
-  // their own: 114 to 109 us; 16 of 6 queries over 4992 and up to 700: 72 to 65.
+  // their own: 94 to 86 us; 16 of 6 queries over 4992 and up to 700: 56 to 49.  Without shared
+  // keys 26 to 28 (64 sequences of up to 1000).
   const bool once = j.pos0 > 0;
   auto issue = [&](const void* pool, uint32_t to) {
     const char* p = static_cast<const char*>(pool);
     if (once) {
 #pragma unroll
       for (int i = 0; i < NI; ++i)
-        lds_dma16_once(uniform(p + off[i & 1]), voff + 64 * (i >> 1), to + (i >> 1) * 2048 + (i & 1) * 1024);
+        lds_dma16_once(uniform(p + off[i & 1]), voff + 64 * (i >> 1),
+                       to + (i >> 1) * 2048 + (i & 1) * 1024);
     } else {
 #pragma unroll
       for (int i = 0; i < NI; ++i)
-        lds_dma16(uniform(p + off[i & 1]), voff + 64 * (i >> 1), to + (i >> 1) * 2048 + (i & 1) * 1024);
+        lds_dma16(uniform(p + off[i & 1]), voff + 64 * (i >> 1),
+                  to + (i >> 1) * 2048 + (i & 1) * 1024);
     }
   };
 
@@ -992,7 +995,8 @@ __device__ void attend_f32(const Args& a, const Job& j, char* lds_all, float2* l
 #pragma unroll
     for (int s = 0; s < 4; ++s)
 #pragma unroll
-      for (int dq = 0; dq < DQ; ++dq) x.v[s][dq] = ldg_f32x4(v + (4 * gk + s) * D + 4 * n + 64 * dq);
+      for (int dq = 0; dq < DQ; ++dq)
+        x.v[s][dq] = ldg_f32x4(v + (4 * gk + s) * D + 4 * n + 64 * dq);
   };
   f32x4 acc[DQ][4];
 #pragma unroll
@@ -1131,7 +1135,8 @@ __device__ __forceinline__ Place place_of(const Args& a, const Schedule& s, int 
   p.h = uniform(div_small(u, per_head, inv_head));
   const int in = u - p.h * per_head;
   int before = 0;  // segments that start at or before `in`: the last of them is not empty
-  for (int i = 0; i < n; i += 64) before += __popcll(__ballot(i + lane < n && s.off[i + lane] <= in));
+  for (int i = 0; i < n; i += 64)
+    before += __popcll(__ballot(i + lane < n && s.off[i + lane] <= in));
   p.seg = uniform(before) - 1;
   const bool shared = p.seg < groups;
   const int units = uniform(s.off[p.seg + 1]) - uniform(s.off[p.seg]);
@@ -1159,7 +1164,9 @@ enum Split { kWhole, kRuns, kGroups };
 
 // Row tile t of a call without shared segments: head by head, the last rows first (under a
 // causal mask they see the most keys), sequence by sequence.  With a.cols > 1 XCDs to a head
-// (kWhole) each takes every a.cols-th row tile, so that they have as many keys to see.
+// (kWhole) each takes every a.cols-th row tile, so that they have as many keys to see (6
+// causal prompts of 701 queries, 16 heads over 4, d 64: 42 to 37 us; 10 % of that lost where
+// the prompts' own lengths even them out).
 struct Tile {
   int h, b, rt;
 };
@@ -1187,8 +1194,11 @@ __device__ __forceinline__ Tile tile_of(const Args& a, int t) {
 // In kWhole a CU has one or two row tiles at a time, so the longest ones decide.  An XCD's row
 // tiles are ranked by the keys that they see, the most first, and the second half of those
 // that run together the other way round: its longest one shares its CU with its shortest.
-// Returns this workgroup's tile of [t0, t0 + n).
-constexpr int kCusXcd = 32;
+// 64 sequences of up to 1000 tokens, 4 heads a key head (8 of them), d 128: 29 to 26 us; 80 of
+// them 41 to 36; with more than kMostRanked row tiles an XCD it loses what the order of the
+// heads keeps in the L2 (causal prompts, 132 of them: 48 to 50).  Returns this workgroup's tile
+// of [t0, t0 + n).
+constexpr int kCusXcd = 32, kMostRanked = 128;
 template <int W>
 __device__ int ranked_tile(const Args& a, Schedule& s, int t0, int n, int in_xcd) {
   const int i = threadIdx.x;
@@ -1256,7 +1266,7 @@ prefix_attention_kernel(const Args a) {
   if constexpr (whole) {
     const int n = min(slots_xcd, nt - xcd * slots_xcd);
     if (in_xcd >= n) return;
-    if (n > kCusXcd && n <= 256)
+    if (n > kCusXcd && n <= kMostRanked)
       t = uniform(ranked_tile<W>(a, s, xcd * slots_xcd, n, in_xcd));
   }
   if (rounds) {
@@ -1376,9 +1386,10 @@ prefix_attention_kernel(const Args a) {
 
 // Joins the partial rows of every row that has some: those of the shared keys, then those
 // of its own, in key order.  Workgroup (x, h, b) takes `chunk` rows of a (sequence, key
-// head), in the order of its own segment; PG groups of D / 4 threads share a row, each taking every PG-th part, four parts'
-// loads at a time, and their sums are joined in group order.  Latency-bound: two loads in
-// turn.
+// head), in the order of its own segment; PG groups of D / 4 threads share a row, each taking
+// every PG-th part, four parts' loads at a time, and their sums are joined in group order.
+// Latency-bound: lengths and parts, then the rows (64 samples of 32 heads with 18 parts each
+// 6.4 us; 10.7 MB of them).
 constexpr int kCombineThreads = 256;
 template <int D, typename T, int PG>
 __global__ void __launch_bounds__(kCombineThreads)
@@ -1473,18 +1484,21 @@ prefix_combine_kernel(const Args a, int chunk) {
 
 // How a call is cut up, by its row tiles and by the keys that a table row has room for.
 // Every row tile whole, in a workgroup of its own, saves finding the runs and the joining
-// kernel (some 5 us); a workgroup of eight waves reads one row tile's keys at twice the rate
-// of one of four, where there is a CU for each.  Timed over 4 to 800 row tiles of sequences
-// of 1 to 4000 tokens (us; whole with 4 waves, runs with 4, whole with 8, runs with 8):
-//   bf16, d 128,  24 row tiles, up to 1000 keys  13.8  20.3  12.6  17.3
-//                                  4000          42.0  21.3  28.9  19.8
-//                256               1000          17.8  26.1  18.1  27.1
-//                512               1000          29.6  38.4  32.4  39.1
-//                                  2000          65.7  67.9  64.9  63.1
-//   bf16, d 64,  128               2000          19.8  20.0  14.1  20.2
-//                512               2000          26.9  35.2  28.4  38.3
-//   fp32, d 128,  24               1000          24.7  28.3  24.1  21.8
-//                512               4000         217.7 197.4 203.8 193.0
+// kernel (some 5 us); a workgroup of eight waves reads one row tile's keys at up to twice the
+// rate of one of four, where there is a CU for each.  Row tiles of few rows, sequences of 1 to
+// n tokens, and of n each (us: whole with 4 waves, runs with 4, whole with 8, runs with 8):
+//   bf16, d 128,  24 row tiles, 1-2000    18  20  14  17        1-4000   36  21  28  19
+//                160            1-2000    22  26  21  25          4000   59  70  67  69
+//                272            1-2000    31  37  33  36          4000  144 111 141 110
+//                384            1-4000    78  87  78  82          4000  150 151 153 147
+//                512            1-4000    95 110 106 104          8000  345 352 348 353
+//                576            1-4000   105 122 116 116          8000  433 401 446 398
+//   bf16, d 64,  160            1-4000    30  25  21  26          4000   40  37  32  38
+//                512            1-4000    52  60  57  60          4000   92  97  95  98
+//   fp32, d 128,  24            1-1000    24  28  23  21        1-4000   81  30  74  24
+//                192            1-1500    38           39          1500   55           69
+//                272            1-2000    64  69  64  66          2000  129 114 134 115
+//                512            1-4000   182 199 195 193          4000  350 354 349 354
 struct Plan {
   Split split;
   int waves;
@@ -1518,17 +1532,20 @@ Plan plan_of(const Args& a, const PrefixCall& p, bool bf16, int d) {
             (tiles >= kPrefixSlots / 2 && (p.causal ? keys <= 4096 || keys <= 2ll * p.S
                                                     : keys <= 4096 && tiles <= kPrefixSlots));
   } else if (tiles <= kPrefixSlots / 2) {
-    whole = bf16 ? keys <= 2048 : keys * d <= 1 << 16;
-  } else {
-    whole = keys <= (row < 256 ? 2048 : 1024);
+    whole = !bf16 ? keys * d <= 1 << 16 || (tiles >= kPrefixSlots / 4 && keys <= 1024) ||
+                        (tiles >= 192 && keys <= 1536)
+                  : keys <= 2048 || (row < 256 && tiles >= kPrefixSlots / 4 && keys <= 4096);
+  } else {  // the nearer they come to a row tile a slot, the better
+    whole = keys <= (tiles >= 384 ? 4096 : bf16 ? 2048 : 1536) ||
+            (tiles >= 448 && tiles <= kPrefixSlots && keys <= 8192);
   }
   // with eight times as many row tiles as slots these even out by themselves
   whole = whole || (a.G == 0 && tiles >= 8 * kPrefixSlots);
-  // workgroups without 128-row tiles have eight waves: whole row tiles while there is a CU for
-  // each, runs but for many row tiles of short rows or few keys
+  // workgroups without 128-row tiles have eight waves: whole row tiles up to half the CUs (all
+  // with short rows), runs but for many row tiles of short rows or few keys
   const bool few = !many || (whole && !many_own);
   const bool eight =
-      few && (whole ? tiles <= kPrefixSlots / 2
+      few && (whole ? tiles * row <= 1 << 15
                     : tiles <= 64 || (row >= 256 && (tiles <= kPrefixSlots / 2 || keys > 1024)));
   return {whole ? kWhole : a.G > 0 ? kGroups : kRuns, eight ? 8 : 4};
 }
@@ -1593,7 +1610,7 @@ void launch_prefix_attention(const PrefixCall& p, int dtype, int d, char* ws, hi
   const Plan plan = plan_of(a, p, dtype == 0, d);
   const Split split = plan.split;
   const bool wide = plan.waves == 8;
-  if (split == kWhole) a.G = 0;
+  if (split != kGroups) a.G = 0;  // the joining kernel looks for what the split left
   a.cols = split == kWhole && a.Hkv < kXcds ? ceil_div(kXcds, a.Hkv) : 1;
   a.longer = a.nrto % a.cols;
   a.by_longer = divisor(a.nrto / a.cols + 1);
