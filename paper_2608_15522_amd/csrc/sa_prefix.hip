@@ -1512,9 +1512,9 @@ Plan plan_of(const Args& a, const PrefixCall& p, bool bf16, int d) {
   if (a.G > 0) {
     // reading shared tokens for each sequence: only for so few keys that the caches make up
     // for it.  8 key heads, whole against shared: 64 sequences of 960 + up to 900 tokens at
-    // d 128 35 against 49 us, of 1920 + up to 900 45 against 50, of 3840 + up to 64 47 against
-    // 32; with 24 key heads 114 against 93, 146 against 96 and 133 against 44.
-    whole = bf16 ? keys <= 2048 && tiles * keys <= 1 << 20
+    // d 128 32 against 44 us, of 1920 + up to 900 42 against 46, of 3840 + up to 64 45 against
+    // 29; with 24 key heads, d 64, 448 + up to 400 29 against 38, 960 + up to 900 64 against 55.
+    whole = bf16 ? keys <= 2048 && tiles * keys * d <= 1 << 27
                  : keys * d <= 1 << 17 && tiles * keys * d <= 1 << 25;
   } else if (many_own) {
     // 2048 queries at d 128, whole against runs (us): a workgroup that is alone on its CU goes

@@ -267,6 +267,36 @@ def test_larger_calls(dtype, B, Hq, Hkv, S, d, shared, lo, hi, page, causal):
         assert torch.equal(o, again[0]) and torch.equal(lse, again[1]), "run to run"
 
 
+@pytest.mark.parametrize("dtype,B,Hq,Hkv,S,d,lo,hi", [
+    ("bf16", 7, 16, 4, 410, 64, 0, 500),      # two XCDs to a head, an odd number of row tiles
+    ("bf16", 5, 3, 3, 2600, 128, 0, 400),     # three
+    ("bf16", 6, 5, 1, 700, 64, 1, 300),       # eight
+    ("bf16", 2, 1, 1, 200, 64, 0, 90),        # fewer row tiles than XCDs
+    ("bf16", 24, 8, 8, 70, 64, 0, 1200),
+    ("f32", 9, 4, 4, 130, 64, 0, 200),
+    ("f32", 30, 10, 5, 9, 128, 0, 150),
+    ("bf16", 40, 8, 8, 1, 128, 0, 700),       # one token or none
+    ("bf16", 11, 24, 3, 33, 128, 0, 260),
+    ("bf16", 140, 4, 4, 1, 64, 0, 2000)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_sequences_with_unequal_numbers_of_queries(dtype, B, Hq, Hkv, S, d, lo, hi, causal):
+    """From none to S queries a sequence, behind lo to hi older tokens: row tiles without a
+    query, their order among XCDs and workgroups, runs and rounds without them."""
+    print(f"case queries {dtype} B={B} Hq={Hq}/{Hkv} S={S} d={d} causal={causal}", flush=True)
+    rng = random.Random(B * S)
+    q_len = [rng.choice([0, 1, S // 3, S // 2, S - 1, S, S]) for _ in range(B)]
+    q_len[-1] = S
+    lens = [n + rng.randint(lo, hi) for n in q_len]
+    q, kp, vp, table = make(B, lens, Hq, Hkv, S, d, 32, dtype)
+    want = reference(q, kp, vp, table, lens, d ** -0.5, causal, q_len)
+    check(q, kp, vp, table, lens, d ** -0.5, q_len=q_len, causal=causal, want=want)
+    q_len = [S - n % 2 for n in range(B)]  # nearly all of them
+    lens = [max(n, S) for n in lens]
+    q, kp, vp, table = make(B, lens, Hq, Hkv, S, d, 64, dtype)
+    want = reference(q, kp, vp, table, lens, d ** -0.5, causal, q_len)
+    check(q, kp, vp, table, lens, d ** -0.5, q_len=q_len, causal=causal, want=want)
+
+
 def reference(q, kp, vp, table, lens, scale, causal, q_len=None):
     """pages.paged_attention on the GPU, a sequence at a time (fp64)."""
     B, Hq, S, d = q.shape
