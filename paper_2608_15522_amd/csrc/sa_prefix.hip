@@ -700,6 +700,21 @@ __device__ void attend_many(const Args& a, const Job& j, char* lds) {
     return mx;
   };
 
+  // rows of V that no row of the workgroup sees may hold anything, NaN too: zeros
+  auto clear = [&](int t) {
+    const int rr = 16 * wave + (lane >> 2);
+    if (run0 + kTile * t + rr >= most || none(t, wave)) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+        *reinterpret_cast<u32x4*>(vbuf(t) + i * 4096 + rr * 64 + (lane & 3) * 16) =
+            u32x4{0u, 0u, 0u, 0u};
+    }
+    wait_lds();
+  };
+  // A wave without rows copies its share of the tiles and computes nothing: one sequence of 24
+  // rows in a last row tile leaves three waves idle.
+  const bool idle = j.row0 + 32 * wave >= j.rows;
+
   f32x16 acc[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) acc[dt] = zero16();
@@ -723,10 +738,12 @@ __device__ void attend_many(const Args& a, const Job& j, char* lds) {
     }
     wait_dma();
     __syncthreads();
-    qk(0, sc0, sc1);
-    if (T_full < 1) mask(0, sc0, sc1);
-    mx_cur = tile_max(sc0, sc1);
-    wait_lds();
+    if (!idle) {
+      qk(0, sc0, sc1);
+      if (T_full < 1) mask(0, sc0, sc1);
+      mx_cur = tile_max(sc0, sc1);
+      wait_lds();
+    }
     __syncthreads();  // every wave has read K(0) before iteration 0 refills its buffer
   }
   auto rescale = [&]() {
@@ -754,17 +771,7 @@ __device__ void attend_many(const Args& a, const Job& j, char* lds) {
   // repeated into the free buffers.
   auto iteration = [&](int t) {
     const size_t off2 = t + 2 < T ? look(t + 2) : off1;
-    if (t >= T_full) {
-      // rows of V that no row of the workgroup sees may hold anything, NaN too: zeros
-      const int rr = 16 * wave + (lane >> 2);
-      if (run0 + kTile * t + rr >= most || none(t, wave)) {
-#pragma unroll
-        for (int i = 0; i < NI; ++i)
-          *reinterpret_cast<u32x4*>(vbuf(t) + i * 4096 + rr * 64 + (lane & 3) * 16) =
-              u32x4{0u, 0u, 0u, 0u};
-      }
-      wait_lds();
-    }
+    if (t >= T_full) clear(t);
     __syncthreads();
     rescale();
     f32x16 sn0, sn1;
@@ -901,6 +908,24 @@ __device__ void attend_many(const Args& a, const Job& j, char* lds) {
   };
 
   const int T_main = T_full == T ? T : (T_full > 1 ? T_full - 1 : 0);
+  if (idle) {
+    for (int t = 0; t < T; ++t) {
+      const size_t off2 = t + 2 < T ? look(t + 2) : off1;
+      if (t >= T_main) {
+        if (t >= T_full) clear(t);
+        __syncthreads();
+      }
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        lds_dma16(uniform(kp + off2) + 64 * i, voff, kdst(t) + i * 4096);
+        lds_dma16(uniform(vp + off1) + 64 * i, voff, vdst(t + 1) + i * 4096);
+      }
+      off1 = off2;
+      wait_dma();
+      __syncthreads();
+    }
+    return;
+  }
   int t = 0;
   for (; t + 1 < T_main; t += 2) {
     main_iter(t, sc0, sc1, sn_0, sn_1);
