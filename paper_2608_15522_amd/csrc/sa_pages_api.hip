@@ -60,9 +60,17 @@ bool prefix_sizes_ok(int B, int Hq, int Hkv, int S, int d, int dtype, int n_grou
 }
 
 bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-  const char* x = static_cast<const char*>(a);
-  const char* y = static_cast<const char*>(b);
-  return x < y + nb && y < x + na;
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y ? na > y - x : nb > x - y;  // an end may lie behind the last address
+}
+
+// Bytes of a pool; Hkv and n_pages may be any ints.
+int pool_bytes(const char* fn, int n_pages, int Hkv, int page, size_t row_bytes, size_t* bytes) {
+  const size_t heads = static_cast<size_t>(n_pages) * Hkv;  // below 2^62
+  if (__builtin_mul_overflow(heads, page * row_bytes, bytes))
+    return fail(SA_ERR_UNSUPPORTED, "%s: n_pages=%d pages of Hkv=%d heads are too large", fn,
+                n_pages, Hkv);
+  return SA_OK;
 }
 
 }  // namespace
@@ -102,7 +110,8 @@ int sa_pages_write(const void* k, const void* v, void* k_pages, void* v_pages,
   SA_TRY(check_tensor(fn, "missing", missing, false, 4));
   const int row_bytes = d * (dtype == SA_BF16 ? 2 : 4);
   const size_t rows = static_cast<size_t>(B) * Hkv * S * row_bytes;
-  const size_t pool = static_cast<size_t>(n_pages) * Hkv * page * row_bytes;
+  size_t pool;
+  SA_TRY(pool_bytes(fn, n_pages, Hkv, page, row_bytes, &pool));
   if (overlap(k_pages, pool, v_pages, pool))
     return fail(SA_ERR_INVALID_ARG, "%s: k_pages and v_pages overlap", fn);
   if (overlap(k, rows, k_pages, pool) || overlap(v, rows, k_pages, pool) ||
@@ -228,7 +237,8 @@ int sa_prefix_attention(const void* q, const void* k_pages, const void* v_pages,
   SA_TRY(check_tensor(fn, "q_len", q_len, false, 4));
   const size_t e = dtype == SA_BF16 ? 2 : 4;
   const size_t rows = static_cast<size_t>(B) * Hq * S * d * e;
-  const size_t pool = static_cast<size_t>(n_pages) * Hkv * page * d * e;
+  size_t pool;
+  SA_TRY(pool_bytes(fn, n_pages, Hkv, page, d * e, &pool));
   if (overlap(o, rows, q, rows) || overlap(o, rows, k_pages, pool) ||
       overlap(o, rows, v_pages, pool))
     return fail(SA_ERR_INVALID_ARG, "%s: o overlaps an input", fn);

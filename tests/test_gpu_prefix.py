@@ -58,11 +58,11 @@ def f64(x):
 
 def check(q, kp, vp, table, lens, scale, shared=None, q_len=None, causal=False, want=None):
     """Runs the call on poisoned outputs and compares it, with the table as given and with
-    rows that have room for 5000 tokens more (the length of the rows decides how the work is
+    rows that have room for 10000 tokens more (the length of the rows decides how the work is
     cut up); returns (o, lse) of the first."""
     if want is None:
         want = pages.paged_attention(f64(q), f64(kp), f64(vp), table, lens, scale, q_len, causal)
-    wide = [list(r) + [-1] * (5000 // kp.shape[2]) for r in table]
+    wide = [list(r) + [-1] * (10000 // kp.shape[2]) for r in table]
     check_one(q, kp, vp, wide, [min(n, len(table[0]) * kp.shape[2]) for n in lens], scale, shared,
               q_len, causal, want)
     return check_one(q, kp, vp, table, lens, scale, shared, q_len, causal, want)
@@ -482,3 +482,97 @@ def test_random_calls(seed):
     again = check(q, kp, vp, table, lens, d ** -0.5, shared=claim, q_len=q_len, causal=causal,
                   want=full)
     assert torch.equal(o, again[0]) and torch.equal(lse, again[1]), "run to run"
+
+
+# row tiles whole, in runs, in rounds and runs, of groups; both forms and types
+SPLITS = [("bf16", 3, 2, 1, 5, 64, None, 300, 0), ("bf16", 3, 2, 1, 5, 64, None, 300, 9000),
+          ("bf16", 4, 8, 4, 60, 128, None, 700, 0), ("bf16", 4, 8, 4, 60, 128, None, 700, 9000),
+          ("f32", 70, 8, 8, 2, 64, None, 150, 9000), ("bf16", 6, 4, 2, 3, 128, [128, 256], 400, 9000),
+          ("bf16", 40, 4, 2, 3, 64, [512], 100, 9000), ("f32", 6, 4, 2, 3, 64, [128, 64], 400, 9000)]
+
+
+def case(split, seed=0):
+    """A call of SPLITS: its arguments, without outputs and workspace, and those of make."""
+    dtype, B, Hq, Hkv, S, d, shared, hi, room = split
+    rng = random.Random(seed)
+    lens = [(shared[b * len(shared) // B] if shared else 0) + rng.randint(0, hi) for b in range(B)]
+    q, kp, vp, table = make(seed, lens, Hq, Hkv, S, d, 64, dtype, shared or ())
+    table = [list(r) + [-1] * (room // 64) for r in table]
+    args = [q, kp, vp, torch.tensor(table, **I32), torch.tensor(lens, **I32), d ** -0.5]
+    return args, dict(shared_len=None if shared is None else torch.tensor(shared, **I32)), lens, table
+
+
+@pytest.mark.parametrize("split", range(len(SPLITS)))
+def test_workspaces_of_any_content(split):
+    """The bits that a workspace is left with, those of NaN and of large numbers too, change
+    nothing; queries that are not there may be NaN."""
+    print(f"case workspace {SPLITS[split]}", flush=True)
+    args, kw, lens, _ = case(SPLITS[split], split)
+    q = args[0]
+    B, Hq, S, d = q.shape
+    rng = random.Random(split)
+    q_len = [rng.randint(0, S) for _ in range(B)]
+    for b, n in enumerate(q_len):
+        q[b, :, n:] = float("nan")
+    for causal in (False, True):
+        need = sa.sa_prefix_attention_workspace(B, Hq, args[1].shape[1], S, d, q.dtype,
+                                                0 if kw["shared_len"] is None else
+                                                kw["shared_len"].numel())
+        seen = []
+        for fill in (0, 0xff, 0x7f, 1):
+            ws = torch.full((need,), fill, dtype=torch.uint8, device="cuda")
+            o, lse = torch.full_like(q, 7.0), torch.full((B, Hq, S), 7.0, device="cuda")
+            sa.sa_prefix_attention(*args, **kw, q_len=torch.tensor(q_len, **I32), causal=causal,
+                                   o=o, lse=lse, ws=ws)
+            torch.cuda.synchronize()
+            seen.append((o, lse))
+        assert all(torch.isfinite(seen[0][0][b, :, :n]).all() for b, n in enumerate(q_len))
+        assert all((seen[0][0][b, :, n:] == 7).all() for b, n in enumerate(q_len))
+        for o, lse in seen[1:]:
+            assert torch.equal(o, seen[0][0]) and torch.equal(lse, seen[0][1])
+
+
+def test_calls_on_two_streams_at_once():
+    """Every kind of call beside every other, each with a workspace of its own."""
+    calls = [case(s, 50 + i) for i, s in enumerate(SPLITS)]
+    alone = []
+    for args, kw, _, _ in calls:
+        alone.append(sa.sa_prefix_attention(*args, **kw, want_lse=True))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for turn in range(3):
+        got = [None] * len(calls)
+        for i in range(len(calls)):
+            k = (i * 3 + turn) % len(calls)
+            with torch.cuda.stream(streams[i % 2]):
+                got[k] = sa.sa_prefix_attention(*calls[k][0], **calls[k][1], want_lse=True)
+        torch.cuda.synchronize()
+        for (o, lse), (p, m) in zip(alone, got):
+            assert torch.equal(o, p) and torch.equal(lse, m)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_numbers_of_queries_outside_their_range(dtype):
+    """q_len counts as 0 below and as S above."""
+    lens = [40, 41, 130, 7, 64]
+    q, kp, vp, table = make(9, lens, 4, 2, 6, 64, 16, dtype)
+    want = pages.paged_attention(f64(q), f64(kp), f64(vp), table, lens, 0.125, [0, 6, 3, 6, 0], True)
+    o, lse = torch.full_like(q, 7.0), torch.full((5, 4, 6), 7.0, device="cuda")
+    sa.sa_prefix_attention(q, kp, vp, torch.tensor(table, **I32), torch.tensor(lens, **I32), 0.125,
+                           q_len=torch.tensor([-5, 13, 3, 2 ** 31 - 1, -2 ** 31], **I32),
+                           causal=True, o=o, lse=lse)
+    a, m = check(q, kp, vp, table, lens, 0.125, q_len=[0, 6, 3, 6, 0], causal=True, want=want)
+    assert torch.equal(o, a) and torch.equal(lse, m)
+
+
+@pytest.mark.parametrize("Hkv", [1, 63])
+def test_as_many_sequences_and_heads_as_there_may_be(Hkv):
+    B = 1024
+    print(f"case most sequences Hkv={Hkv}", flush=True)
+    lens = [b % 35 for b in range(B)]
+    q, kp, vp, table = make(3, lens, 2 * Hkv, Hkv, 1, 64, 16, "bf16")
+    want = reference(q, kp, vp, table, [max(n, 1) for n in lens], 0.125, False)
+    for b, n in enumerate(lens):
+        if n == 0:
+            want[0][b], want[1][b], want[2][b] = 0.0, -np.inf, 0.0
+    check(q, kp, vp, table, lens, 0.125, want=want)

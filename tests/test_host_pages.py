@@ -74,6 +74,8 @@ INVALID += [
     (_write, dict(v_pages=FAKE + 4096), ARG, "k_pages and v_pages overlap"),
     (_write, dict(k=FAKE + 4096), ARG, "overlaps the pages"),
     (_write, dict(missing=FAKE + 2), ARG, "missing is not 4"),
+    (_write, dict(B=1, S=1, n_pages=2 ** 31 - 1, Hkv=2 ** 29, d=128, dtype=1, page=128), UNS,
+     "heads are too large"),
     (_write, dict(B=16384, Hkv=4096, S=64), UNS, "too large"),
     (_fork, dict(n=0), ARG, "n=0"), (_fork, dict(n=5), ARG, "n=5"),
     (_fork, dict(src=None), ARG, "src is NULL"), (_fork, dict(dst=None), ARG, "dst is NULL"),
