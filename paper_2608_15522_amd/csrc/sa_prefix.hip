@@ -1142,9 +1142,10 @@ __device__ __forceinline__ int run_at(const Runs& r, int x) {
   while (c + 1 < r.n && run_begin(r, c + 1) <= x) ++c;
   return c;
 }
-// Whether a row tile may be cut at its unit k.
-__device__ __forceinline__ bool cuts(int cost, int per, int k) {
-  return k >= cost + kSnap && k <= per - kSnap;
+// Where a cut at unit k of a row tile goes.
+__device__ __forceinline__ int cut_at(int cost, int per, int k) {
+  if (k >= cost + kSnap && k <= per - kSnap) return k;
+  return k < cost + kSnap ? 0 : per;
 }
 
 // Where unit u lies: its head, segment, row tile, the units of the row tile before it, and
@@ -1311,53 +1312,53 @@ prefix_attention_kernel(const Args a) {
     total = uniform(__shfl(upto, 63, 64));
     t += in_xcd;
   }
-  // The run: units [u, stop) of the call or, after the rounds, of the XCD's rest.  The first
-  // two turns of the loop move its ends to where row tiles may be cut.
+  // The run: units [u, stop) of the call or, after the rounds, of the XCD's rest, both ends
+  // moved to where row tiles may be cut.
   const int my = rounds ? in_xcd : slot;
   const Runs runs = runs_of(total, rounds ? slots_xcd : gridDim.x);
-  int u = 0, stop = 0, turn = 2;
+  int u = 0, stop = 0;
+  bool moved = true;  // u
   if (!whole && my < runs.n && total > 0) {
     u = uniform(run_begin(runs, my));
     stop = my + 1 < runs.n ? uniform(run_begin(runs, my + 1)) : total;
-    turn = 0;
+    moved = false;
   }
-  for (;; ++turn) {
+  for (;;) {
     Place p;
     int take = 0, last = 0;  // slots behind this one that hold parts of a row tile begun here
-    if (!GROUPS && turn >= 2 && t < (rounds ? rest : whole ? end : 0)) {
+    if (!GROUPS && t < (rounds ? rest : whole ? end : 0)) {
       const Tile x = tile_of<whole>(a, uniform(t));
       p = Place{x.h, x.b, x.rt, 0, row_units(a.co, whole ? 0 : s.len[x.b])};
       take = p.per;
       t = whole ? end : t + slots_xcd;
     } else {
-      const int x = turn == 1 ? stop : u;
-      if (turn >= 2 && u >= stop) break;
-      if (turn == 1 && stop == total) continue;
+      if (u >= stop) break;
       if (rounds) {
-        const int i = uniform(__popcll(__ballot(upto <= x)));
+        const int i = uniform(__popcll(__ballot(upto <= u)));
         p.per = __builtin_amdgcn_readlane(per_l, i);
-        p.k = x - (__builtin_amdgcn_readlane(upto, i) - p.per);
+        p.k = u - (__builtin_amdgcn_readlane(upto, i) - p.per);
         const Tile y = tile_of<whole>(a, rest + i);
         p.h = y.h;
         p.seg = y.b;
         p.rt = y.rt;
       } else if constexpr (!whole) {
-        p = place_of<GROUPS>(a, s, per_head, inv_head, x);
+        p = place_of<GROUPS>(a, s, per_head, inv_head, u);
       }
       const int cost = p.seg < groups ? a.cp : a.co;
-      if (turn < 2) {
-        int y = x;
-        if (!cuts(cost, p.per, p.k)) y = p.k < cost + kSnap ? x - p.k : x - p.k + p.per;
-        if (turn == 0)
-          u = uniform(y);
-        else
-          stop = uniform(y);
-        continue;
+      if (!moved) {
+        moved = true;
+        const int k = cut_at(cost, p.per, p.k);
+        u = uniform(u + k - p.k);
+        if (k > p.k) continue;  // another row tile
+        p.k = k;
       }
-      take = min(stop - u, p.per - p.k);
+      take = uniform(min(stop - u + p.k, p.per));
+      if (take < p.per) take = uniform(cut_at(cost, p.per, take));
+      take -= p.k;
+      if (take == 0) break;  // the next run takes the row tile from its start
       // those whose runs begin inside the row tile
-      if (take < p.per && p.k == 0) last = run_at(runs, u + p.per - kSnap) - my;
-      u += take;
+      if (p.k + take < p.per && p.k == 0) last = run_at(runs, u + p.per - kSnap) - my;
+      u = p.k + take < p.per ? stop : u + take;
     }
     const int cost = p.seg < groups ? a.cp : a.co;
     Job j;

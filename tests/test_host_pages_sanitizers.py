@@ -24,7 +24,7 @@ pytestmark = pytest.mark.skipif(not os.path.exists(HIPCC), reason="hipcc not fou
 
 
 @pytest.fixture(scope="module")
-def checker(tmp_path_factory):
+def built(tmp_path_factory):
     out = tmp_path_factory.mktemp("pages_asan")
     san = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
            "-Xarch_host", "-fno-sanitize-recover=all"]
@@ -67,8 +67,8 @@ def line(call, **kw):
                                    else str(int(v)) for v in args.values()])
 
 
-def test_refusals_launch_nothing(checker):
-    got = run(checker, [line(call, **kw) for call, kw, _, _ in INVALID])
+def test_refusals_launch_nothing(built):
+    got = run(built, [line(call, **kw) for call, kw, _, _ in INVALID])
     for (call, kw, code, needle), (rc, launches, text) in zip(INVALID, got):
         assert rc == code & 0xffffffffffffffff, (call.name, kw, rc)  # printed as 64 bits
         assert launches == 0 and needle in text, (call.name, kw, text)
@@ -80,12 +80,12 @@ def accepted(rc, launches, text):
                               and "kernel launch failed" in text)
 
 
-def test_accepted_calls_launch_once(checker):
-    for got, call in zip(run(checker, [line(c) for c in CALLS]), CALLS):
+def test_accepted_calls_launch_once(built):
+    for got, call in zip(run(built, [line(c) for c in CALLS]), CALLS):
         assert accepted(*got), (call.name, got)
 
 
-def test_ends_of_the_types(checker):
+def test_ends_of_the_types(built):
     """Every number alone and every two together at the ends of 32 bits: refused or accepted,
     without overflow."""
     lines = []
@@ -97,17 +97,17 @@ def test_ends_of_the_types(checker):
                 if call is _copy and "page_bytes" in kw:
                     kw["page_bytes"] = kw["page_bytes"] & (2 ** 64 - 1)
                 lines.append(line(call, **kw))
-    for args, got in zip(lines, run(checker, lines)):
+    for args, got in zip(lines, run(built, lines)):
         rc, launches, text = got
         nothing = args.startswith("sa_pages_copy") and (rc, launches, text) == (0, 0, "-")  # n = 0
         refused = rc in REFUSALS and launches == 0 and text != "-"
         assert accepted(*got) or refused or nothing, (args, got)
 
 
-def test_workspace_sizes_agree_with_the_library(checker):
+def test_workspace_sizes_agree_with_the_library(built):
     cases = [(B, Hq, Hkv, S, d, t, g) for B in (1, 4, 1023, INT_MAX) for Hq, Hkv in
              ((1, 1), (8, 2), (INT_MAX, 1), (INT_MAX, INT_MAX), (3, 2)) for S in (1, 33, 262144)
              for d in (64, 128, 96) for t in (0, 1, 7) for g in (0, 1, B, INT_MIN)]
-    got = run(checker, ["sa_prefix_attention_workspace " + " ".join(map(str, c)) for c in cases])
+    got = run(built, ["sa_prefix_attention_workspace " + " ".join(map(str, c)) for c in cases])
     for c, (size, _, _) in zip(cases, got):
         assert size == sa.lib().sa_prefix_attention_workspace(*c), c
