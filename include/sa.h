@@ -549,9 +549,10 @@ int sa_pages_copy(void* pools, int n_pools, int n_pages, size_t page_bytes,
  * causal = 1 it sees the tokens up to its own only.  Query head i reads key head
  * i / (Hq / Hkv).  A row that sees no key outputs zeros and lse = -inf, as does
  * one whose every logit is -inf; rows from q_len[b] on are left as they were.
- * Tokens whose table entry is no page are left out, and nothing that lies in a
- * page behind a sequence's last token is used.  A token that a query does not
- * see by causality weighs 0 in it: its value must be finite.
+ * Tokens whose table entry is no page, or that lie behind the table row, are
+ * left out (the queries' positions stay), and nothing that lies in a page behind
+ * a sequence's last token is used.  A token that a query does not see by causality
+ * weighs 0 in it: its value must be finite.
  *
  * The B sequences are n_groups groups of B / n_groups neighbours.  shared_len[g]
  * says how many leading tokens the sequences of group g have in common, in the

@@ -102,7 +102,8 @@ def paged_attention(q, k_pages, v_pages, table, lens, scale, q_len=None, causal=
     lse = np.full((B, Hq, S), np.nan)
     for b in range(B):
         new = S if q_len is None else int(q_len[b])
-        at = [t for t in range(max(int(lens[b]), 0)) if 0 <= table[b][t // page] < n_pages]
+        held = min(max(int(lens[b]), 0), len(table[b]) * page)  # later tokens have no page
+        at = [t for t in range(held) if 0 <= table[b][t // page] < n_pages]
         pos = np.array(at, dtype=np.int64)
         ids = np.array([table[b][t // page] for t in at], dtype=np.int64)
         for h in range(Hq):

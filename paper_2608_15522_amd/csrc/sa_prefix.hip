@@ -104,6 +104,9 @@ __device__ __forceinline__ int seq_tokens(const Args& a, int b) {
   const int len = a.seq_len[b];
   return len < 0 ? 0 : static_cast<int>(len < cap ? len : cap);
 }
+// What the queries' positions count from: a length beyond the table row leaves out the tokens
+// that have no page, and the newest queries stay where they are.
+__device__ __forceinline__ int seq_end(const Args& a, int b) { return max(a.seq_len[b], 0); }
 __device__ __forceinline__ int seq_queries(const Args& a, int b) {
   return a.q_len != nullptr ? min(max(a.q_len[b], 0), a.S) : a.S;
 }
@@ -173,7 +176,8 @@ __device__ void build_schedule(const Args& a, Schedule& s) {
     s.nq[b] = nq;
     if (!GROUPS) atomicMax(&s.most, row_units(a.co, len));
     if (GROUPS && len > 0)
-      atomicMin(&s.sh[group_of(a, b)], a.causal ? max(min(len - nq + 1, len), 0) : len);
+      atomicMin(&s.sh[group_of(a, b)],
+                a.causal ? max(min(seq_end(a, b) - max(nq - 1, 0), len), 0) : len);
   }
   __syncthreads();
   if constexpr (GROUPS) {
@@ -320,7 +324,7 @@ __device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xC07F);
 // Last key position that a row sees, plus one.
 __device__ __forceinline__ int row_end(const Args& a, const Job& j, const Row& r) {
   if (!a.causal || j.shared) return j.pos1;
-  return min(j.pos1, seq_tokens(a, r.b) - j.nq + r.query + 1);
+  return min(j.pos1, seq_end(a, r.b) - j.nq + r.query + 1);
 }
 
 __device__ __forceinline__ float natural_lse(float m, float l) {
@@ -628,7 +632,7 @@ __device__ void attend_many(const Args& a, const Job& j, char* lds) {
   const int run0 = j.pos0 + kTile * j.t0, run1 = min(j.pos1, j.pos0 + kTile * j.t1);
   int most = run1, least = run1;       // the furthest and the nearest end of the tile's rows
   if (a.causal && !j.shared) {
-    const int q0 = seq_tokens(a, j.b0) - j.nq + 1, last = min(j.row0 + kManyRows, j.rows) - 1;
+    const int q0 = seq_end(a, j.b0) - j.nq + 1, last = min(j.row0 + kManyRows, j.rows) - 1;
     most = min(run1, q0 + a.by_R.by(last));
     least = min(run1, q0 + a.by_R.by(j.row0));
   }
@@ -1235,7 +1239,7 @@ __device__ int ranked_tile(const Args& a, Schedule& s, int t0, int n, int in_xcd
     int keys = row0 < rows ? seq_tokens(a, x.b) : 0;
     if (a.causal && row0 < rows) {
       const int last = min(row0 + a.TRo, rows) - 1;
-      keys = max(keys - nq + a.by_R.by(last) + 1, 0);
+      keys = max(min(keys, seq_end(a, x.b) - nq + a.by_R.by(last) + 1), 0);
     }
     mine = static_cast<uint32_t>(ceil_div(keys, kTile)) << 8 | static_cast<uint32_t>(255 - i);
   }
