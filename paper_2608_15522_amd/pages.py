@@ -20,6 +20,7 @@ class KVPages:
     kv         [layers,2,n_pages,Hkv,page,d]: keys and values of every layer
     page_table, seq_len, page_ref: as the C calls document them
     missing, fork_missing: [1] i32, of the last reserve and of the last fork
+    new        [B] i32: what the last reserve was given, for the writes behind it
     """
 
     def __init__(self, B, max_tokens, n_pages, Hkv, d, page=64, layers=1,
@@ -29,18 +30,23 @@ class KVPages:
         self.kv = torch.empty(layers, 2, n_pages, Hkv, page, d, dtype=dtype, device=device)
         self.page_table = e(B, -(-max_tokens // page)).fill_(-1)
         self.seq_len, self.page_ref = e(B), e(n_pages)
-        self.missing, self.fork_missing = e(1), e(1)
+        self.missing, self.fork_missing, self.new = e(1), e(1), e(B)
         self._pools = self.kv.view(2 * layers, n_pages, Hkv, page, d)
 
     def reserve(self, n_new):
         """Room for n_new[b] more tokens of every sequence (all or nothing)."""
-        return sa.sa_pages_reserve(self.page_table, self.seq_len, self.page_ref, n_new,
-                                   self.page, missing=self.missing)
+        sa.sa_pages_reserve(self.page_table, self.seq_len, self.page_ref, n_new, self.page,
+                            missing=self.missing)
+        torch.mul(n_new, 1, out=self.new)
+        return self.missing
 
     def write(self, layer, k, v, n_new=None):
-        """Keys and values [B,Hkv,S,d] of the tokens reserved last, if they were."""
+        """Keys and values [B,Hkv,S,d] of the tokens reserved last, if they were: the first
+        new[b] rows of each sequence (or n_new[b], what reserve was given).  Every layer's
+        before the next fork or free."""
         sa.sa_pages_write(k, v, self.kv[layer, 0], self.kv[layer, 1], self.page_table,
-                          self.seq_len, n_new=n_new, missing=self.missing)
+                          self.seq_len, n_new=self.new if n_new is None else n_new,
+                          missing=self.missing)
 
     def attend(self, layer, q, scale, **options):
         """sa_prefix_attention of q [B,Hq,S,d] over the layer's pages; returns (o, lse)."""
