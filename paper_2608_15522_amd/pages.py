@@ -4,8 +4,8 @@
 (with torch), as ``LayerPlan`` does for one layer of the sparse path; its methods enqueue
 the library's kernels on the current stream and never wait for the GPU.  What may fail
 for want of pages (``reserve``, ``fork``) returns how many lack, a device tensor that the
-caller reads when it likes: until then a reservation that failed has changed nothing, and
-``write`` writes nothing.
+caller reads when it likes: until then a reservation that failed has changed nothing,
+``write`` writes nothing, and ``new``, the tokens that the reservation brought, is 0.
 """
 from __future__ import annotations
 
@@ -20,7 +20,8 @@ class KVPages:
     kv         [layers,2,n_pages,Hkv,page,d]: keys and values of every layer
     page_table, seq_len, page_ref: as the C calls document them
     missing, fork_missing: [1] i32, of the last reserve and of the last fork
-    new        [B] i32: what the last reserve was given, for the writes behind it
+    new        [B] i32: tokens of each sequence that the last reserve made room for (0 for
+               all if it failed), to be passed on as q_len of their queries
     """
 
     def __init__(self, B, max_tokens, n_pages, Hkv, d, page=64, layers=1,
@@ -31,13 +32,15 @@ class KVPages:
         self.page_table = e(B, -(-max_tokens // page)).fill_(-1)
         self.seq_len, self.page_ref = e(B), e(n_pages)
         self.missing, self.fork_missing, self.new = e(1), e(1), e(B)
+        self._done = torch.zeros(1, dtype=torch.bool, device=device)
         self._pools = self.kv.view(2 * layers, n_pages, Hkv, page, d)
 
     def reserve(self, n_new):
         """Room for n_new[b] more tokens of every sequence (all or nothing)."""
         sa.sa_pages_reserve(self.page_table, self.seq_len, self.page_ref, n_new, self.page,
                             missing=self.missing)
-        torch.mul(n_new, 1, out=self.new)
+        torch.eq(self.missing, 0, out=self._done)
+        torch.mul(n_new, self._done, out=self.new)
         return self.missing
 
     def write(self, layer, k, v, n_new=None):
