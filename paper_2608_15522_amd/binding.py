@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import math
 import os
 from typing import Optional
 
@@ -629,7 +630,7 @@ def sa_pages_copy(pools, src, dst):
     _expect(dst, "dst", (n,), torch.int32)
     _here(pools, src, dst)
     _check(lib().sa_pages_copy(
-        _ptr(pools), n_pools, n_pages, pools.stride(1) * pools.element_size(),
+        _ptr(pools), n_pools, n_pages, math.prod(pools.shape[2:]) * pools.element_size(),
         _ptr(src) if n > 0 else None, _ptr(dst) if n > 0 else None, n, _stream()))
     return pools
 
