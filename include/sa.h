@@ -436,6 +436,7 @@ int sa_cache_indicator(const void* y_v, const void* y_v_hat,
  *                     -1 = none
  *   seq_len           [B] i32: tokens of each sequence (negative counts as 0)
  *   page_ref          [n_pages] i32: how many table entries name the page; 0 = free
+ *                     (n_pages <= 2^30 in the calls that take it)
  * page in {16, 32, 64, 128}; max_pages * page <= 2^30; B <= 16384 (the
  * attention: B + n_groups <= 1024, B * Hkv <= 65535).  Every list lives on the
  * device, so the calls can be captured into a HIP graph and follow the lists'

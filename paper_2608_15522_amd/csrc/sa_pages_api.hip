@@ -30,7 +30,13 @@ int check_cache(const char* fn, int B, int max_pages, int n_pages, int page, int
   return SA_OK;
 }
 
-int check_table(const char* fn, const int32_t* page_table, const int32_t* page_ref) {
+// The planning kernels go through the owner counts in steps of 16384 pages, in 32 bits.
+constexpr int kMaxPages = 1 << 30;
+
+int check_table(const char* fn, const int32_t* page_table, const int32_t* page_ref,
+                int n_pages) {
+  if (n_pages > kMaxPages)
+    return fail(SA_ERR_UNSUPPORTED, "%s: n_pages=%d exceeds %d", fn, n_pages, kMaxPages);
   SA_TRY(check_tensor(fn, "page_table", page_table, true, 4));
   SA_TRY(check_tensor(fn, "page_ref", page_ref, true, 4));
   return SA_OK;
@@ -82,7 +88,7 @@ int sa_pages_reserve(int32_t* page_table, int32_t* seq_len, int32_t* page_ref,
                      int32_t* missing, void* stream) {
   const char* fn = "sa_pages_reserve";
   SA_TRY(check_cache(fn, B, max_pages, n_pages, page, sa::kMaxSequences));
-  SA_TRY(check_table(fn, page_table, page_ref));
+  SA_TRY(check_table(fn, page_table, page_ref, n_pages));
   SA_TRY(check_tensor(fn, "seq_len", seq_len, true, 4));
   SA_TRY(check_tensor(fn, "n_new", n_new, true, 4));
   SA_TRY(check_tensor(fn, "missing", missing, true, 4));
@@ -129,7 +135,7 @@ int sa_pages_fork(int32_t* page_table, int32_t* seq_len, int32_t* page_ref, cons
   SA_TRY(check_cache(fn, B, max_pages, n_pages, page, sa::kMaxSequences));
   if (n < 1 || n > B)
     return fail(SA_ERR_INVALID_ARG, "%s: n=%d outside [1, B=%d]", fn, n, B);
-  SA_TRY(check_table(fn, page_table, page_ref));
+  SA_TRY(check_table(fn, page_table, page_ref, n_pages));
   SA_TRY(check_tensor(fn, "seq_len", seq_len, true, 4));
   SA_TRY(check_tensor(fn, "src", src, true, 4));
   SA_TRY(check_tensor(fn, "dst", dst, true, 4));
@@ -147,7 +153,7 @@ int sa_pages_free(int32_t* page_table, int32_t* seq_len, int32_t* page_ref, cons
   SA_TRY(check_cache(fn, B, max_pages, n_pages, page, sa::kMaxSequences));
   if (n < 1 || n > sa::kMaxSequences)
     return fail(SA_ERR_INVALID_ARG, "%s: n=%d outside [1, %d]", fn, n, sa::kMaxSequences);
-  SA_TRY(check_table(fn, page_table, page_ref));
+  SA_TRY(check_table(fn, page_table, page_ref, n_pages));
   SA_TRY(check_tensor(fn, "seq_len", seq_len, true, 4));
   SA_TRY(check_tensor(fn, "seqs", seqs, true, 4));
   sa::launch_pages_free(page_table, seq_len, page_ref, seqs, n, B, max_pages, n_pages, page,
@@ -159,7 +165,7 @@ int sa_pages_compact(int32_t* page_table, int32_t* page_ref, int B, int max_page
                      int32_t* move_src, int32_t* move_dst, int32_t* counts, void* stream) {
   const char* fn = "sa_pages_compact";
   SA_TRY(check_cache(fn, B, max_pages, n_pages, 16, sa::kMaxSequences));  // reads no tokens
-  SA_TRY(check_table(fn, page_table, page_ref));
+  SA_TRY(check_table(fn, page_table, page_ref, n_pages));
   SA_TRY(check_tensor(fn, "move_src", move_src, n_pages > 1, 4));
   SA_TRY(check_tensor(fn, "move_dst", move_dst, n_pages > 1, 4));
   SA_TRY(check_tensor(fn, "counts", counts, true, 4));

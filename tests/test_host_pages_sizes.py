@@ -1,5 +1,5 @@
-"""Host side of the paged calls, on the CPU: the sizes that the binding hands over.  No call
-here reaches a kernel."""
+"""Host side of the paged calls, on the CPU: the sizes that the binding hands over, and
+numbers of pages near the end of their type.  No call here reaches a kernel."""
 import os
 
 import pytest
@@ -7,6 +7,7 @@ import torch
 
 import paper_2608_15522_amd as sa
 from paper_2608_15522_amd import binding
+from test_host_pages import _compact, _fork, _free, _reserve
 
 pytestmark = pytest.mark.skipif(not os.path.exists(binding.LIB_PATH),
                                 reason="libsa.so not built")
@@ -35,3 +36,12 @@ def test_bytes_of_a_page(monkeypatch, pools, page_bytes):
     sa.sa_pages_copy(pools, pairs, pairs)
     (args,) = seen
     assert args[1:4] == (pools.shape[0], pools.shape[1], page_bytes)
+
+
+@pytest.mark.parametrize("call", [_reserve, _fork, _free, _compact], ids=lambda c: c.name)
+@pytest.mark.parametrize("n_pages", [2 ** 30 + 1, 2 ** 31 - 16384, 2 ** 31 - 1])
+def test_more_pages_than_can_be_counted_are_refused(call, n_pages):
+    """The kernels take 16384 page numbers a step, in 32 bits: the number behind the last step
+    has to fit."""
+    assert call(n_pages=n_pages) == sa.SA_ERR_UNSUPPORTED
+    assert call.name in sa.sa_last_error() and f"n_pages={n_pages}" in sa.sa_last_error()
