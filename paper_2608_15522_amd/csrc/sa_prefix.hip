@@ -92,7 +92,6 @@ struct Args {
   int longer;                 // of these, those that take by_longer.d row tiles; the others
   Div by_longer, by_least;    // by_least.d
   int nrtp, nrto;             // row tiles of a segment (an own one with S queries)
-  float inv_nrtp;
   float* full;                // [2][B * Hq * S][D] partial rows of whole row tiles
   float2* full_ml;            // [2][B * Hq * S]
   float* piece;               // [2 slots][TR][D] partial rows of shared row tiles
@@ -113,9 +112,10 @@ __device__ __forceinline__ int seq_queries(const Args& a, int b) {
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-// x / y for 0 <= x < 2^30, 0 < y, inv = 1.f / y.  The product is off by less than one for
-// quotients below 2^21; the kernel's start is bound by cold instruction fetches, and an
-// integer division is some thirty of them.
+// x / y for 0 <= x < 2^30, 0 < y, inv = 1.f / y, and quotients below 2^21: x, y, inv and the
+// product are each rounded by 2^-24 relatively, so the product is off by less than one.  The
+// kernel's start is bound by cold instruction fetches, and an integer division is some thirty
+// of them.
 __device__ __forceinline__ int div_small(int x, int y, float inv) {
   int q = static_cast<int>(static_cast<float>(x) * inv);
   q -= q * y > x;
@@ -162,6 +162,12 @@ __device__ __forceinline__ int own_tiles(const Args& a, const Schedule& s, int b
   return a.q_len == nullptr ? a.nrto : (a.R * s.nq[b] + a.TRo - 1) >> a.lTRo;
 }
 
+// Tokens of sequence b behind the shared ones.
+template <bool GROUPS>
+__device__ __forceinline__ int own_keys(const Args& a, const Schedule& s, int b) {
+  return GROUPS ? max(s.len[b] - s.sh[group_of(a, b)], 0) : s.len[b];
+}
+
 template <int W, bool GROUPS>
 __device__ void build_schedule(const Args& a, Schedule& s) {
   constexpr int NT = W * kWave;
@@ -193,8 +199,7 @@ __device__ void build_schedule(const Args& a, Schedule& s) {
   auto units = [&](int i) {
     if (i < groups) return s.sh[i] == 0 ? 0 : a.nrtp * row_units(a.cp, s.sh[i]);
     const int b = i - groups;
-    return own_tiles(a, s, b) *
-           row_units(a.co, GROUPS ? max(s.len[b] - s.sh[group_of(a, b)], 0) : s.len[b]);
+    return own_tiles(a, s, b) * row_units(a.co, own_keys<GROUPS>(a, s, b));
   };
   int sum = 0;
   for (int i = i0; i < i1; ++i) sum += units(i);
@@ -1169,11 +1174,11 @@ __device__ __forceinline__ Place place_of(const Args& a, const Schedule& s, int 
     before += __popcll(__ballot(i + lane < n && s.off[i + lane] <= in));
   p.seg = uniform(before) - 1;
   const bool shared = p.seg < groups;
-  const int units = uniform(s.off[p.seg + 1]) - uniform(s.off[p.seg]);
-  const int tiles = shared ? a.nrtp : a.nrto == 1 ? 1 : uniform(own_tiles(a, s, p.seg - groups));
-  p.per = units;
-  if (tiles > 1)
-    p.per = uniform(div_small(units, tiles, shared ? a.inv_nrtp : 1.f / static_cast<float>(tiles)));
+  const int b = p.seg - groups;
+  if (GROUPS && shared)
+    p.per = row_units(a.cp, uniform(s.sh[p.seg]));
+  else
+    p.per = row_units(a.co, uniform(own_keys<GROUPS>(a, s, b)));
   const int x = in - uniform(s.off[p.seg]);
   p.rt = uniform(div_small(x, p.per, 1.f / static_cast<float>(p.per)));
   p.k = x - p.rt * p.per;
@@ -1622,7 +1627,6 @@ void launch_prefix_attention(const PrefixCall& p, int dtype, int d, char* ws, hi
   a.parts = reinterpret_cast<int2*>(ws + w.parts);
   a.nrtp = w.groups > 0 ? ceil_div(a.N * a.RS, a.TRp) : 0;
   a.nrto = ceil_div(a.RS, a.TRo);
-  a.inv_nrtp = a.nrtp > 0 ? 1.f / static_cast<float>(a.nrtp) : 0.f;
   a.by_B = divisor(a.B);
   a.by_tiles = divisor(a.B * a.nrto);
   a.full = reinterpret_cast<float*>(ws + w.full);

@@ -1,5 +1,6 @@
 """sa_prefix_attention at the ends of its lengths, against the fp64 oracle and against
 sums that are exact."""
+import math
 import random
 
 import pytest
@@ -61,3 +62,26 @@ def test_longest_length_that_a_number_holds(form):
         want = sa.sa_prefix_attention(q, kp, vp, t, torch.full((B,), cap, **I32), d ** -0.5,
                                       shared_len=sh, q_len=n, want_lse=True)
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("dtype,S,n_pages", [("bf16", 384, (1 << 23) - 1), ("f32", 48, (1 << 23) - 2),
+                                             ("bf16", 1, 1 << 23)])
+def test_nearly_as_many_tokens_as_there_may_be(dtype, S, n_pages):
+    """2^30 tokens, all in one page but for the last 128; with more queries than one, three row
+    tiles of 2^24 + 2 units of work each, a number whose threefold no float holds.  The keys
+    of the first page are 0, so that every weight before the last page is the same and every
+    sum exact; those of the last one outweigh them all."""
+    page, d, t = 128, 64, {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+    print(f"case {n_pages} pages {dtype} S={S}", flush=True)
+    kp, vp = torch.zeros(2, 1, page, d, dtype=t, device="cuda"), torch.ones(2, 1, page, d, dtype=t,
+                                                                          device="cuda")
+    q = torch.zeros(1, 1, S, d, dtype=t, device="cuda")
+    q[..., 0], kp[1, ..., 0], vp[1] = 1.0, 240.0, 2.0
+    table = torch.zeros(1, 1 << 23, **I32)
+    table[0, n_pages - 1] = 1
+    o, lse = sa.sa_prefix_attention(q, kp, vp, table, torch.tensor([n_pages * page], **I32), 0.125,
+                                    want_lse=True)
+    # scores of 0 and 30: the others weigh n_pages / e^30 < 1e-6 of the last page, and O differs
+    # from 2 by as much (bf16: 2); 30 log2(e) is off by 4 * 2^-24 of itself at most
+    assert (o.float() - 2).abs().max() <= 2e-6
+    assert (lse - (30 + math.log(128))).abs().max() <= 2e-5
