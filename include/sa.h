@@ -468,8 +468,8 @@ int sa_pages_reserve(int32_t* page_table, int32_t* seq_len, int32_t* page_ref,
  * sequence b is token seq_len[b] - n_new[b] + s.
  *
  *   k, v       [B,Hkv,S,d] in dtype; not overlapping the pages
- *   n_new      [B] i32, at most S count; NULL = S for every sequence.  Rows from
- *              n_new[b] on are not read, and tokens without a page not written.
+ *   n_new      [B] i32, more than S count as S; NULL = S for every sequence.  Rows
+ *              from n_new[b] on are not read, and tokens without a page not written.
  *   missing    [1] i32, nullable: what sa_pages_reserve returned for these tokens;
  *              nothing is written unless it is 0 (the last n_new[b] tokens would
  *              be older ones)
@@ -486,7 +486,8 @@ int sa_pages_write(const void* k, const void* v, void* k_pages, void* v_pages,
  * The full pages are shared (an owner more each).  A partial last page gets a
  * fresh page, so that both sequences can go on writing: the pair (copy_src[i],
  * copy_dst[i]) is to be copied in every pool with sa_pages_copy before either is
- * written; both are -1 where there is nothing to copy.  An entry is left out if
+ * written; both are -1 where there is nothing to copy (copy_src alone, or no page,
+ * where src's table entry is none).  An entry is left out if
  * its src has no tokens or more than its table row has room for, if its dst has
  * some, or if it names a sequence outside [0,B); of several entries with one dst
  * the first counts.  Fresh pages are the lowest free ones, in the order of the

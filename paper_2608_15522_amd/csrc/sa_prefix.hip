@@ -472,8 +472,8 @@ __device__ void attend_few(const Args& a, const Job& j, char* lds_all, float2* l
   };
   // Own keys behind shared ones are read once, by this job, and leave the caches to the
   // shared ones (nt): 64 samples of 4 query heads over 16384 shared tokens and up to 2000 of
-  // their own: 94 to 86 us; 16 of 6 queries over 4992 and up to 700: 56 to 49.  Without shared
-  // keys 26 to 28 (64 sequences of up to 1000).
+  // their own: 94 to 86 us; 16 of 6 queries each over 4992 and up to 700: 46 to 40.  Without
+  // shared keys 26 to 28 (64 sequences of up to 1000).
   const bool once = j.pos0 > 0;
   auto issue = [&](const void* pool, uint32_t to) {
     const char* p = static_cast<const char*>(pool);
@@ -995,7 +995,9 @@ __device__ void attend_many(const Args& a, const Job& j, char* lds) {
 //                  and K[n]; the result leaves it with keys 4gk .. 4gk + 3 of query n;
 //   O^T += V^T P^T with k slot gk of step r standing for key 4gk + r, and row i of channel
 //                  tile (dq, e) for channel 64dq + 4i + e.
-// Weights are taken down by 2^-8, the slack of the running max, so that none exceeds 1.
+// Weights are taken down by 2^-8, the slack of the running max, so that none exceeds 1.  Under a
+// causal mask every row tile goes through all keys of its segment, also those that none of its
+// rows sees (the form of many rows stops at the last that one does).
 constexpr int kF32Keys = 16;
 template <int D, int W>
 __device__ void attend_f32(const Args& a, const Job& j, char* lds_all, float2* lds_ml) {
@@ -1191,17 +1193,20 @@ __device__ __forceinline__ Place place_of(const Args& a, const Schedule& s, int 
 // whole row tiles, in rounds of all slots of an XCD, and only the rest is cut: the workgroups
 // of a round go through a head's keys side by side, so that these come from the XCD's L2.  16
 // heads of 4 x 1024 queries over 16000 keys (a whole row tile a slot) run at 920 TFLOP/s, 20
-// heads cut into equal runs at 740.  kGroups: runs over shared and own segments.  Each is a
-// kernel of its own, since a short call waits for its instructions as long as for its data: 4
-// sequences of 316 tokens, 8 heads of d 64, 6.4 us in a kernel of kWhole alone, 7.8 in one of
-// all three.
+// heads cut into equal runs at 740.  5 x 1024 queries, 16 heads, d 128, over 8000 keys in the
+// mean, the longest 1.0, 1.2, 1.3 and 1.5 times that: 404, 390, 373 and 370 us in runs, 321, 347,
+// 359 and 376 in rounds; 130 single tokens, 4 heads, over 3000: 148, 153, 152 and 153 in runs,
+// 148, 155, 160 and 171 in rounds.  kGroups: runs over shared and own segments.  Each is a kernel
+// of its own, since a short call waits for its instructions as long as for its data: 4 sequences
+// of 316 tokens, 8 heads of d 64, 6.4 us in a kernel of kWhole alone, 7.8 in one of all three.
 enum Split { kWhole, kRuns, kGroups };
+constexpr float kUneven = 1.25f;  // the longest row tile to the mean, for rounds at most
 
 // Row tile t of a call without shared segments: head by head, the last rows first (under a
 // causal mask they see the most keys), sequence by sequence.  With a.cols > 1 XCDs to a head
 // (kWhole) each takes every a.cols-th row tile, so that they have as many keys to see (6
-// causal prompts of 701 queries, 16 heads over 4, d 64: 42 to 37 us; 10 % of that lost where
-// the prompts' own lengths even them out).
+// causal prompts of 701 queries each, 16 heads over 4, d 64: 39 to 34 us behind 512 tokens
+// each, 43 to 38 behind 512 to 1014).
 struct Tile {
   int h, b, rt;
 };
@@ -1229,8 +1234,8 @@ __device__ __forceinline__ Tile tile_of(const Args& a, int t) {
 // In kWhole a CU has one or two row tiles at a time, so the longest ones decide.  An XCD's row
 // tiles are ranked by the keys that they see, the most first, and the second half of those
 // that run together the other way round: its longest one shares its CU with its shortest.
-// 64 sequences of up to 1000 tokens, 4 heads a key head (8 of them), d 128: 29 to 26 us; 80 of
-// them 41 to 36; with more than kMostRanked row tiles an XCD it loses what the order of the
+// 64 sequences of up to 1000 tokens, 4 heads a key head (8 of them), d 128: 36 to 31 us; 80 of
+// them 41 to 38; with more than kMostRanked row tiles an XCD it loses what the order of the
 // heads keeps in the L2 (causal prompts, 132 of them: 48 to 50).  Returns this workgroup's tile
 // of [t0, t0 + n).
 constexpr int kCusXcd = 32, kMostRanked = 128;
@@ -1291,12 +1296,12 @@ prefix_attention_kernel(const Args a) {
         for (int i = threadIdx.x; i < a.G; i += W * kWave) a.shared_out[i] = s.sh[i];
     } else {
       rounds = nt >= static_cast<int>(gridDim.x) &&
-               uniform(s.most) <= 1.25f * static_cast<float>(total) / static_cast<float>(nt);
+               uniform(s.most) <= kUneven * static_cast<float>(total) / static_cast<float>(nt);
     }
   }
   // Rounds: row tiles [t, end) of the XCD, slots_xcd at a time.  What remains then, less than
-  // one row tile a slot, is kept a row tile a lane (slots_xcd is 64): units `per_l`, `upto`
-  // with those of the lanes before.
+  // one row tile a slot, is kept a row tile a lane (slots_xcd is at most 64): units `per_l`,
+  // `upto` with those of the lanes before.
   int t = slot, end = nt, rest = 0, per_l = 0, upto = 0;
   if constexpr (whole) {
     const int n = min(slots_xcd, nt - xcd * slots_xcd);
@@ -1517,7 +1522,10 @@ prefix_combine_kernel(const Args a, int chunk) {
   }
 }
 
-// How a call is cut up, by its row tiles and by the keys that a table row has room for.
+// How a call is cut up, by its row tiles and by the keys that a table row has room for: the
+// lengths are on the device, so a table wider than its sequences is cut up as for longer ones
+// (6 causal prompts of up to 701 queries, d 64: whole row tiles, 28 us, or with a table four
+// times as wide runs, 36; 4 x 1 token over 316, 8 heads: 11, and 13 sixteen times as wide).
 // Every row tile whole, in a workgroup of its own, saves finding the runs and the joining
 // kernel (some 5 us); a workgroup of eight waves reads one row tile's keys at up to twice the
 // rate of one of four, where there is a CU for each.  Row tiles of few rows, sequences of 1 to
@@ -1549,6 +1557,10 @@ Plan plan_of(const Args& a, const PrefixCall& p, bool bf16, int d) {
     // for it.  8 key heads, whole against shared: 64 sequences of 960 + up to 900 tokens at
     // d 128 32 against 44 us, of 1920 + up to 900 42 against 46, of 3840 + up to 64 45 against
     // 29; with 24 key heads, d 64, 448 + up to 400 29 against 38, 960 + up to 900 64 against 55.
+    // fp32, one token, 8 key heads, d 64: 16 sequences of 960 + up to 64 14.5 against 15.3, of
+    // 1920 + up to 64 23 against 15.5 (18 in four waves); 64 of 448 + up to 64 16.0 against
+    // 18.8, of 960 + up to 64 25 against 19; d 128: 16 of 448 + up to 64 14.5 against 18.2, of
+    // 960 + up to 64 24.5 against 20.7.
     whole = bf16 ? keys <= 2048 && tiles * keys * d <= 1 << 27
                  : keys * d <= 1 << 17 && tiles * keys * d <= 1 << 25;
   } else if (many_own) {
@@ -1574,10 +1586,26 @@ Plan plan_of(const Args& a, const PrefixCall& p, bool bf16, int d) {
     whole = keys <= (tiles >= 384 ? 4096 : bf16 ? 2048 : 1536) ||
             (tiles >= 448 && tiles <= kPrefixSlots && keys <= 8192);
   }
-  // with eight times as many row tiles as slots these even out by themselves
+  // With eight times as many row tiles as slots these even out by themselves, if no sequence is
+  // much longer than the others: the longest row tile is one workgroup.  512 sequences of 8
+  // heads, d 128, whole against runs: 1000 tokens each 360 and 370 us, 1 to 2000 367 and 375, one
+  // of 20000 478 and 389, one of 100000 1294 and 445; 4 x 16384 queries, 8 heads, d 64, 16384
+  // keys 2273 and 2279, causal 1171 and 1233; 64 x 1024 queries, 8 heads, d 128, 1024 to 4096
+  // keys 1187 and 1118, causal 1005 and 950.
   whole = whole || (a.G == 0 && tiles >= 8 * kPrefixSlots);
-  // workgroups without 128-row tiles have eight waves: whole row tiles up to half the CUs (all
-  // with short rows), runs but for many row tiles of short rows or few keys
+  // Workgroups without 128-row tiles have eight waves: whole row tiles up to half the CUs (all
+  // with short rows), runs but for many row tiles of short rows or few keys.  Four waves against
+  // eight, us, sequences of 1 to n tokens:
+  //   whole, n = 1000 (fp32 500)      row tiles   64        128       256       320
+  //     bf16, d 128                           13.3 12.5  13.7 13.1  16.1 16.7  19.8 21.8
+  //     bf16, d 64                             9.6  9.6  11.2  9.5  11.8 10.5  13.2 14.8
+  //     fp32, d 128                           15.0 15.7  15.4 16.3  17.6 19.0  21.5 22.3
+  //     fp32, d 64                             9.6  9.6  10.2 10.2  11.1 11.8  13.0 15.7
+  //   runs, n = 4000 (fp32 2000)      row tiles   48        96        128       512
+  //     bf16, d 128                           22.5 20.1  29.0 28.9  36.7 36.2   106  102
+  //     bf16, d 64                            17.6 15.8  19.4 19.0  20.9 21.4    59   58
+  //     fp32, d 128                           29.0 22.4  32.2 28.8  38.0 37.8   109  107
+  //     fp32, d 64                            19.3 16.5  20.5 19.5  21.7 21.5    59   59
   const bool few = !many || (whole && !many_own);
   const bool eight =
       few && (whole ? tiles * row <= 1 << 15
