@@ -432,7 +432,7 @@ __device__ __forceinline__ void stg16_nt(void* p, u32x4 v) {
 // of one page; a workgroup takes every gridDim.x-th one, 64 list entries looked up at
 // once, so that entries to be skipped (-1: a list filled up to its capacity) cost a
 // lane each and no latency of their own.  Loads and stores are nontemporal: 1.05 GB moved
-// in 201 us, 5.2 TB/s (a plain copy of 2 GiB: 4.9); some 7 % longer with ordinary stores.
+// in 199 us, 5.3 TB/s (a plain copy of 2 GiB: 4.9); some 7 % longer with ordinary stores.
 constexpr int kCopyThreads = 256;
 constexpr int kCopyLoads = 4;  // 16-byte loads in flight a thread
 constexpr int kCopyUnit = kCopyThreads * kCopyLoads * 16;

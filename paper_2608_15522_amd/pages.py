@@ -52,7 +52,11 @@ class KVPages:
                           missing=self.missing)
 
     def attend(self, layer, q, scale, **options):
-        """sa_prefix_attention of q [B,Hq,S,d] over the layer's pages; returns (o, lse)."""
+        """sa_prefix_attention of q [B,Hq,S,d] over the layer's pages; returns (o, lse).
+        q_len: new, or another number of each sequence's last tokens; ws: a workspace that
+        calls one behind the other may share (sa_prefix_attention_workspace bytes, tens of
+        MB; else made for each call).  The groups of shared_len are equal numbers of
+        neighbouring sequences."""
         return sa.sa_prefix_attention(q, self.kv[layer, 0], self.kv[layer, 1], self.page_table,
                                       self.seq_len, scale, **options)
 
