@@ -44,6 +44,9 @@ CALLS = [
     ("f32", 2, 2, 2, 100, 128, 64, 512, 100, 700),
     ("f32", 70, 8, 8, 2, 64, 64, 0, 1500, 1510),
 ]
+# as many queries as there may be
+LONGEST = [("bf16", 1, 1, 1, 262144, 64, 128, 0, 262144, 262144),
+           ("f32", 1, 1, 1, 40000, 64, 32, 0, 40000, 40100)]
 
 
 def lengths(call):
@@ -79,7 +82,7 @@ def tile_values(at, tokens, heads, d, off):
     return v.scatter_(2, c[..., None], amp[:, None, None].expand(tokens, heads, 1))
 
 
-@pytest.mark.parametrize("call", CALLS, ids=lambda c: "-".join(map(str, c)))
+@pytest.mark.parametrize("call", CALLS + LONGEST, ids=lambda c: "-".join(map(str, c)))
 @pytest.mark.parametrize("causal", [False, True])
 def test_every_tile_counts_once(call, causal):
     print(f"case tiles {call} causal={causal}", flush=True)
